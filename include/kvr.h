@@ -75,7 +75,8 @@ enum {
     KVR_E_WORKSPACE = -5,  /* workspace too small or not 256-byte aligned         */
     KVR_E_DOMAIN = -6,     /* device-detected bad sample or index (status word)   */
     KVR_E_HIP = -7,        /* a HIP runtime call failed                           */
-    KVR_E_METHOD = -8      /* unknown method, or an option the method lacks       */
+    KVR_E_METHOD = -8,     /* unknown method, or an option the method lacks       */
+    KVR_E_LAYOUT = -9      /* a type, head size, stride or alignment not supported */
 };
 
 enum { KVR_BRUTE = 0, KVR_SORTED = 1 };   /* kvr_cost_grid methods            */
@@ -361,6 +362,189 @@ int kvr_crossover_statistic(const double *d_wait_s, int64_t n, const kvr_prices 
 int kvr_cost_grid_noalloc(const double *d_wait_s, const int32_t *d_ctx_tokens, int64_t n,
                           const kvr_prices *p, const kvr_policy_grid *g, int32_t method,
                           double *d_cost, int32_t *d_perm, int32_t *d_status, void *hip_stream);
+
+/* ---- The paged KV cache -------------------------------------------------------
+ *
+ * What the retention policies above price by the byte: the keys and values of a
+ * request's context.  Four operators write them (rotating keys by their
+ * positions, and quantising), read them back, and attend over them.
+ *
+ * A cache is a pool of pages; a page holds page_size tokens of every KV head.
+ * The row of one token and head (head_dim elements, adjacent) is at
+ *   data + page * page_stride + head * head_stride + token_in_page * token_stride
+ * and its scale bytes, for the quantised formats, at the same place in the scale
+ * strides.  Keys and values have one set of strides; they may be two
+ * allocations or two parts of one.  Any order of pages, heads and tokens in
+ * memory will do, as long as rows do not overlap.
+ *
+ * Formats.  KVR_KV_BF16 and KVR_KV_FP16 keep 16-bit elements.  KVR_KV_FP8 and
+ * KVR_KV_FP4 cut a row into blocks of 32 elements; a block keeps a scale byte e
+ * for 2^(e - 127) and 32 codes, 8-bit e4m3 or 4-bit e2m1 (the even element in
+ * the low half of its byte).  Writing chooses the smallest exponent for which no
+ * code saturates, at least -110 (2^k * M >= the block's largest magnitude, M =
+ * 448 or 6), and rounds element / 2^k to the nearest code, ties to even.  A
+ * block with a NaN or an infinity keeps scale byte 255 and reads as NaN;
+ * magnitudes beyond 1.75 * 2^127 (e4m3: 1.9375 * 2^127) read as infinities.  A
+ * 128-element row takes 256, 132 or 68 bytes.
+ *
+ * Conventions of these entry points, beside the shared ones above: strides of
+ * activations count elements, those of a cache bytes; the elements of a row are
+ * adjacent; counts may be zero (nothing is launched).  Device-detected errors
+ * (a position outside the table, a slot or page outside the pool, lengths that
+ * do not fit the call) are reported through d_status, device int32[1] or NULL:
+ * the kernels store KVR_E_DOMAIN there and never clear it, and nothing outside
+ * the caller's buffers is touched.  None of them allocates or synchronises. */
+enum { KVR_DT_BF16 = 0, KVR_DT_FP16 = 1, KVR_DT_FP32 = 2 };                   /* activations */
+enum { KVR_KV_BF16 = 0, KVR_KV_FP16 = 1, KVR_KV_FP8 = 2, KVR_KV_FP4 = 3 };    /* cache rows  */
+
+typedef struct {
+    void *k_data, *v_data;      /* device, 16-byte aligned                             */
+    void *k_scale, *v_scale;    /* device, scale bytes; NULL for 16-bit formats        */
+    int64_t page_stride, head_stride, token_stride;                     /* bytes, of 16 */
+    int64_t scale_page_stride, scale_head_stride, scale_token_stride;   /* bytes        */
+    int64_t n_pages;            /* 1 .. 2^31 - 1                                       */
+    int32_t page_size;          /* tokens: a power of two, 16 .. 32,768                */
+    int32_t n_kv_heads;         /* 1 .. 1,024                                          */
+    int32_t head_dim;           /* 64, 96, 128, 192 or 256                             */
+    int32_t format;             /* KVR_KV_*                                            */
+} kvr_kv_cache;                 /* token_stride and scale_token_stride: at most 2^26   */
+
+/* Frequencies of rotary positions.  Pair i of rot_dim / 2 has the frequency
+ * w_i = theta^(-2 i / rot_dim), for contexts longer than trained_len changed by
+ * factor >= 1:
+ *   KVR_ROPE_PLAIN   w_i
+ *   KVR_ROPE_LINEAR  w_i / factor (positions divided by the factor)
+ *   KVR_ROPE_BASE    theta * factor^(rot_dim / (rot_dim - 2)) in theta's place
+ *   KVR_ROPE_TURNS   by the turns n_i = trained_len w_i / 2 pi within the trained
+ *                    length: g w_i + (1 - g) w_i / factor with
+ *                    g = clamp((n_i - low) / (high - low), 0, 1)
+ *   KVR_ROPE_INDEX   the same blend with a ramp in the index: g = 1 - clamp((i - a)
+ *                    / (b - a), 0, 1), a and b the indexes at which the turns are
+ *                    high and low, rounded down and up and kept in
+ *                    [0, rot_dim - 1] (b = a counts as a + 0.001)
+ * cos and sin are multiplied by magnitude (1 for none). */
+enum { KVR_ROPE_PLAIN = 0, KVR_ROPE_LINEAR = 1, KVR_ROPE_BASE = 2, KVR_ROPE_TURNS = 3,
+       KVR_ROPE_INDEX = 4 };
+typedef struct {
+    double theta;          /* > 1                                       */
+    double factor;         /* >= 1 (unused by KVR_ROPE_PLAIN)           */
+    double low, high;      /* turns, 0 < low < high (TURNS, INDEX)      */
+    double trained_len;    /* tokens, > 0 (TURNS, INDEX)                */
+    double magnitude;      /* > 0                                       */
+    int32_t kind;          /* KVR_ROPE_*; an unknown one is KVR_E_METHOD */
+} kvr_rope;
+
+/*
+ * The table of rotary positions: cos and sin of position * w_i, formed in 64 bits
+ * and rounded once.
+ *   d_table   device, float32 [n_pos][2][rot_dim / 2]: cosines, then sines.
+ *   rot_dim   even, 2 .. 256 (KVR_ROPE_BASE: at least 4); n_pos * rot_dim <= 2^38.
+ * A parameter out of its range is KVR_E_GRID.
+ */
+int kvr_rotary_table(const kvr_rope *rope, int32_t rot_dim, int64_t n_pos, float *d_table,
+                     void *hip_stream);
+
+/* Flags of the rotating entry points. */
+enum { KVR_ROTARY_INTERLEAVED = 1,   /* pairs (2i, 2i + 1); else (i, i + rot_dim / 2) */
+       KVR_ROTARY_ADJOINT = 2 };     /* by the negative angle: the gradient           */
+
+/*
+ * Rotary positions of queries, keys or their gradients.
+ *   d_x, d_out     device, dtype [n_tokens][n_heads][head_dim] with the given
+ *                  strides (elements, >= 0).  d_out may be d_x with the same
+ *                  strides; otherwise the two must not overlap.
+ *   d_pos          device, int32 [n_tokens]: row of the table of each token
+ *                  (outside [0, n_pos): KVR_E_DOMAIN, and row 0 is taken).
+ *   d_table, rot_dim, n_pos: as kvr_rotary_table made it; rot_dim <= head_dim, and
+ *                  the elements from rot_dim on are copied.
+ *   Rows that are 16-byte aligned, head_dim a multiple of 8 and rot_dim of 16 (8
+ *   interleaved) go eight elements at a time, others one pair at a time.
+ *   Sizes: n_tokens * n_heads <= 2^31 - 1, n_heads <= 65,536, head_dim <= 65,536.
+ */
+int kvr_rotary(const void *d_x, void *d_out, int32_t dtype, int64_t n_tokens, int32_t n_heads,
+               int32_t head_dim, int64_t x_token_stride, int64_t x_head_stride,
+               int64_t out_token_stride, int64_t out_head_stride, const int32_t *d_pos,
+               const float *d_table, int64_t n_pos, int32_t rot_dim, int32_t flags,
+               int32_t *d_status, void *hip_stream);
+
+/*
+ * Writes keys and values into the cache, quantising them if it is quantised.
+ *   d_k, d_v       device, dtype [n_tokens][n_kv_heads][head_dim], strides in
+ *                  elements; 16-byte aligned rows (else KVR_E_LAYOUT).
+ *   d_slots        device, int64 [n_tokens]: page * page_size + row in the page.
+ *                  Below 0: the token is not written.  Beyond the pool:
+ *                  KVR_E_DOMAIN, not written.  Two tokens of a call must not
+ *                  share a slot.
+ *   d_pos, d_table, n_pos, rot_dim, flags: keys are rotated on the way, in 32 bits
+ *                  (rounded once, by the cache's format); d_table NULL: as they
+ *                  are.  A position outside the table: KVR_E_DOMAIN, not written.
+ *   Sizes: n_tokens * n_kv_heads <= 2^31 - 1.
+ */
+int kvr_cache_write(const kvr_kv_cache *cache, const void *d_k, const void *d_v, int32_t dtype,
+                    int64_t n_tokens, int64_t k_token_stride, int64_t k_head_stride,
+                    int64_t v_token_stride, int64_t v_head_stride, const int64_t *d_slots,
+                    const int32_t *d_pos, const float *d_table, int64_t n_pos, int32_t rot_dim,
+                    int32_t flags, int32_t *d_status, void *hip_stream);
+
+/*
+ * Reads rows of the cache back: d_k, d_v [n_tokens][n_kv_heads][head_dim] in dtype,
+ * from the slots of kvr_cache_write (any number of times the same one).  Below 0:
+ * zeros.  Beyond the pool: zeros and KVR_E_DOMAIN.  The codes' values are exact in
+ * bfloat16 and float32.  Layouts, strides and sizes as kvr_cache_write.
+ */
+int kvr_cache_read(const kvr_kv_cache *cache, const int64_t *d_slots, int64_t n_tokens, void *d_k,
+                   void *d_v, int32_t dtype, int64_t k_token_stride, int64_t k_head_stride,
+                   int64_t v_token_stride, int64_t v_head_stride, int32_t *d_status,
+                   void *hip_stream);
+
+/* Sequences of a kvr_tree_attention call. */
+typedef struct {
+    const int32_t *d_cu_q;      /* device [n_seqs + 1]: first query of each sequence, then n_queries */
+    const int32_t *d_kv_len;    /* device [n_seqs]: its tokens in the cache, the new ones included   */
+    const int32_t *d_pages;     /* device [n_seqs][pages_stride]: its pages, in order                */
+    int64_t pages_stride;       /* elements between the rows of d_pages                              */
+    int64_t max_pages;          /* entries of a row that may be read                                 */
+    int64_t n_queries;          /* new tokens of all sequences                                       */
+    int32_t n_seqs;             /* 0 .. 4,096                                                        */
+    int32_t max_q;              /* bound on a sequence's new tokens, >= 1                            */
+    int32_t max_kv;             /* bound on a sequence's tokens in the cache, >= 1                   */
+} kvr_sequences;
+
+/*
+ * Attention of each sequence's newest tokens over its pages: one token (decoding),
+ * a run of them, or a tree of drafted tokens.  The newest n_b = cu_q[b + 1] -
+ * cu_q[b] of the kv_len[b] cached tokens are the call's queries, so their keys and
+ * values are already in the cache (kvr_cache_write).  Query i sees every token
+ * before the newest n_b, and newest token j
+ *   with d_tree_mask, where bit j % 64 of word j / 64 of its mask row is set (a tree:
+ *   its ancestors and itself; any mask may be given),
+ *   without, where j <= i.
+ *   out[i][h] = sum_j softmax_j(scale * q[i][h] . k_j) v_j,  lse[i][h] = log of the sum
+ * with query head h on KV head h / (n_q_heads / n_kv_heads).  A query that sees
+ * nothing gets zeros and -infinity.  Hidden tokens, and cache rows that are not
+ * in use, may hold anything, NaN and infinities included.
+ *   d_q, d_out     device, dtype (KVR_DT_BF16 or KVR_DT_FP16; a 16-bit cache must
+ *                  have the same) [n_queries][n_q_heads][head_dim], strides in
+ *                  elements, 16-byte aligned rows.  d_out must not overlap d_q.
+ *   d_lse          device, float32 [n_queries][n_q_heads] or NULL.
+ *   d_tree_mask    device, uint64 [n_queries][mask_words] or NULL; mask_words * 64
+ *                  >= max_q.
+ *   Scores, the softmax and the sums are held in float32; the weights are rounded
+ *   to the 16-bit type of the products.
+ *   A sequence whose lengths do not fit (more than max_q or max_kv, fewer cached than
+ *   new tokens, more pages than max_pages) is left out, and a page outside the pool
+ *   is read as page 0: KVR_E_DOMAIN.
+ *   d_ws, ws_bytes  workspace (two-phase sizing as above; contents need not be
+ *                  set).  It may be 0 bytes: then d_ws is not used, any non-NULL
+ *                  256-byte aligned pointer will do.
+ *   Sizes: n_q_heads a multiple of n_kv_heads, max_q * n_q_heads <= 2^24.
+ */
+int kvr_tree_attention(const kvr_kv_cache *cache, const kvr_sequences *seqs, const void *d_q,
+                       int32_t dtype, int32_t n_q_heads, int64_t q_token_stride,
+                       int64_t q_head_stride, const uint64_t *d_tree_mask, int32_t mask_words,
+                       float scale, void *d_out, int64_t out_token_stride, int64_t out_head_stride,
+                       float *d_lse, int32_t *d_status, void *d_ws, size_t *ws_bytes,
+                       void *hip_stream);
 
 /*
  * Instrumentation for benchmarks.  After this call, every kvr_cost_grid,

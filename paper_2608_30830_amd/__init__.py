@@ -12,6 +12,13 @@ import math
 import os
 from typing import Optional, Sequence, Tuple
 
+from . import kv
+from .kv import (KVR_DT_BF16, KVR_DT_FP16, KVR_DT_FP32, KVR_KV_BF16, KVR_KV_FP16,  # noqa: F401
+                 KVR_KV_FP4, KVR_KV_FP8, KVR_ROPE_BASE, KVR_ROPE_INDEX, KVR_ROPE_LINEAR,
+                 KVR_ROPE_PLAIN, KVR_ROPE_TURNS, KVR_ROTARY_ADJOINT, KVR_ROTARY_INTERLEAVED,
+                 KvCache, kv_bytes_per_token, kvr_cache_read, kvr_cache_write, kvr_kv_cache,
+                 kvr_rope, kvr_rotary, kvr_rotary_table, kvr_sequences, kvr_tree_attention)
+
 _PKG = os.path.dirname(os.path.abspath(__file__))
 # KVR_LIBRARY names another build of the same library (e.g. one whose host
 # code is compiled with sanitizers); by default the in-tree build is loaded.
@@ -26,6 +33,7 @@ KVR_E_WORKSPACE = -5
 KVR_E_DOMAIN = -6
 KVR_E_HIP = -7
 KVR_E_METHOD = -8
+KVR_E_LAYOUT = -9
 KVR_BRUTE = 0
 KVR_SORTED = 1
 KVR_RETAIN = 0
@@ -35,7 +43,7 @@ EXPORTS = ("kvr_prices_from_platform", "kvr_cost_grid", "kvr_cost_grid_noalloc",
            "kvr_select_policy", "kvr_bootstrap",
            "kvr_bootstrap_factored", "kvr_eq3_timer", "kvr_capacity_replay",
            "kvr_controller_select", "kvr_crossover_statistic", "kvr_workspace_status",
-           "kvr_set_profile_events", "kvr_status_string")
+           "kvr_set_profile_events", "kvr_status_string") + kv.EXPORTS
 
 
 class kvr_prices(ctypes.Structure):
@@ -111,6 +119,7 @@ def load_library(path: str = LIB_PATH):
     lib.kvr_set_profile_events.restype = ctypes.c_int
     lib.kvr_status_string.argtypes = [ctypes.c_int]
     lib.kvr_status_string.restype = ctypes.c_char_p
+    kv.declare(lib)
     _lib = lib
     return lib
 

@@ -793,6 +793,7 @@ const char *kvr_status_string(int status)
     case KVR_E_DOMAIN: return "bad sample or index detected on the device";
     case KVR_E_HIP: return "HIP runtime error";
     case KVR_E_METHOD: return "unknown method or option not supported by the method";
+    case KVR_E_LAYOUT: return "a type, head size, stride or alignment is not supported";
     default: return "unknown status";
     }
 }

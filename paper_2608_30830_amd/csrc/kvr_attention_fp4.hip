@@ -1,0 +1,13 @@
+// Attention over an e2m1 cache, bfloat16 queries.
+#include "kvr_attention.h"
+
+namespace kvr {
+namespace kv {
+
+hipError_t launch_attention_fp4(const Attention &a, dim3 grid, hipStream_t stream)
+{
+    return launch_dim<KVR_KV_FP4, KVR_DT_BF16>(a, grid, stream);
+}
+
+}  // namespace kv
+}  // namespace kvr

@@ -1,0 +1,98 @@
+// Internal declarations of the paged KV cache's operators: rotary positions,
+// quantised writes and reads, attention of drafted tokens over the cache.
+// These sources are compiled with IEEE NaN handling: a cache holds whatever a
+// model produced, and its unwritten rows hold whatever was in memory.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kvr.h"
+
+namespace kvr {
+namespace kv {
+
+constexpr int kBlock = 32;      // elements that share one scale byte
+constexpr int kMinExp = -110;   // smallest block exponent: every value stays a normal number
+constexpr int kBadScale = 255;  // scale byte of a block that held a NaN or an infinity
+
+inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// A cache as the kernels see it: byte strides, the page size as a shift.
+struct Cache {
+    char *k, *v;
+    uint8_t *ks, *vs;
+    int64_t page_stride, head_stride, token_stride;      // bytes
+    int64_t spage_stride, shead_stride, stoken_stride;   // bytes
+    int64_t n_pages;
+    int32_t page_shift, n_heads, dim, format;
+};
+
+// [tokens][heads][dim] activations: element strides, elements of a row adjacent.
+struct Rows {
+    char *p;
+    int64_t token_stride, head_stride;
+    int32_t dtype;
+};
+
+// cos and sin rows of the positions; t == nullptr: no rotation.
+struct Rotary {
+    const float *t;        // [n_pos][2][rot / 2]
+    const int32_t *pos;    // [tokens]
+    int64_t n_pos;
+    int32_t rot;
+    int32_t interleaved;
+    float sign;            // of the sines: -1 for the adjoint
+};
+
+constexpr int kMaxFreq = 128;   // rot <= 256
+struct Freqs {
+    double w[kMaxFreq];
+};
+
+hipError_t launch_rotary_table(const Freqs &f, double magnitude, int rot, int64_t n_pos,
+                               float *table, hipStream_t stream);
+hipError_t launch_rotary(const Rows &x, const Rows &out, int64_t tokens, int heads, int dim,
+                         const Rotary &r, int *status, hipStream_t stream);
+hipError_t launch_cache_write(const Cache &c, const Rows &k, const Rows &v, int64_t tokens,
+                              const int64_t *slots, const Rotary &r, int *status,
+                              hipStream_t stream);
+hipError_t launch_cache_read(const Cache &c, const Rows &k, const Rows &v, int64_t tokens,
+                             const int64_t *slots, int *status, hipStream_t stream);
+
+constexpr int kStep = 32;        // cached tokens of one step of the attention loop
+constexpr int kMaxSeqs = 4096;
+
+struct Attention {
+    Cache c;
+    Rows q, out;                 // out.dtype == q.dtype
+    float *lse;                  // [n_queries][q_heads] or nullptr
+    const int32_t *cu_q, *kv_len, *pages;
+    const uint64_t *mask;        // [n_queries][words] or nullptr (each token sees the ones before it)
+    int64_t n_queries, pages_stride, max_pages;
+    int32_t n_seqs, q_heads, group, max_q, max_kv, words;
+    float scale2;                // softmax scale * log2(e)
+    // launch plan
+    int32_t row_tiles;           // 16-row tiles of one block
+    int32_t row_blocks;          // blocks that cover max_q * group rows
+    int32_t target;              // parts that all sequences together are cut into, about
+    int32_t max_parts;           // bound on the parts
+    int32_t min_steps;           // steps that a part has at least
+    float *part_o;               // [parts][heads][row_blocks][16 * row_tiles][dim]
+    float *part_ml;              // [parts][heads][row_blocks][16 * row_tiles][2]
+    int *status;
+};
+
+// Fills the launch plan; returns the workspace bytes (0: no sequence is cut).
+size_t plan_attention(Attention &a);
+hipError_t launch_attention(const Attention &a, hipStream_t stream);
+// The attention kernel by cache format and query type.
+hipError_t launch_attention_bf16(const Attention &a, dim3 grid, hipStream_t stream);
+hipError_t launch_attention_fp16(const Attention &a, dim3 grid, hipStream_t stream);
+hipError_t launch_attention_fp8(const Attention &a, dim3 grid, hipStream_t stream);    // bfloat16 q
+hipError_t launch_attention_fp8h(const Attention &a, dim3 grid, hipStream_t stream);   // half q
+hipError_t launch_attention_fp4(const Attention &a, dim3 grid, hipStream_t stream);
+hipError_t launch_attention_fp4h(const Attention &a, dim3 grid, hipStream_t stream);
+
+}  // namespace kv
+}  // namespace kvr

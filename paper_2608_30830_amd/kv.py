@@ -1,0 +1,392 @@
+"""Binding of the paged KV cache's entry points of libkvr: argument marshalling only.
+
+A :class:`KvCache` names the tensors of a cache; ``kvr_cache_write``,
+``kvr_cache_read`` and ``kvr_tree_attention`` work on it, ``kvr_rotary`` on
+activations.  Every call enqueues on torch's current stream (or ``stream``).
+With ``check`` (the default) a call waits and raises on a device-detected error;
+``check=False`` returns without waiting, and an optional ``status`` tensor
+([1] int32, zeroed by the caller) collects KVR_E_DOMAIN.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import Optional
+
+KVR_DT_BF16 = 0
+KVR_DT_FP16 = 1
+KVR_DT_FP32 = 2
+KVR_KV_BF16 = 0
+KVR_KV_FP16 = 1
+KVR_KV_FP8 = 2
+KVR_KV_FP4 = 3
+KVR_ROPE_PLAIN = 0
+KVR_ROPE_LINEAR = 1
+KVR_ROPE_BASE = 2
+KVR_ROPE_TURNS = 3
+KVR_ROPE_INDEX = 4
+KVR_ROTARY_INTERLEAVED = 1
+KVR_ROTARY_ADJOINT = 2
+
+EXPORTS = ("kvr_rotary_table", "kvr_rotary", "kvr_cache_write", "kvr_cache_read",
+           "kvr_tree_attention")
+
+BLOCK = 32   # elements that share a scale byte
+
+
+class kvr_kv_cache(ctypes.Structure):
+    _fields_ = [("k_data", ctypes.c_void_p), ("v_data", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("scale_page_stride", ctypes.c_int64),
+                ("scale_head_stride", ctypes.c_int64), ("scale_token_stride", ctypes.c_int64),
+                ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("format", ctypes.c_int32)]
+
+
+class kvr_rope(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_double), ("factor", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double), ("trained_len", ctypes.c_double),
+                ("magnitude", ctypes.c_double), ("kind", ctypes.c_int32)]
+
+
+class kvr_sequences(ctypes.Structure):
+    _fields_ = [("d_cu_q", ctypes.c_void_p), ("d_kv_len", ctypes.c_void_p),
+                ("d_pages", ctypes.c_void_p), ("pages_stride", ctypes.c_int64),
+                ("max_pages", ctypes.c_int64), ("n_queries", ctypes.c_int64),
+                ("n_seqs", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_kv", ctypes.c_int32)]
+
+
+def declare(lib) -> None:
+    """Argument types of the entry points above."""
+    P, I32, I64, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    C = ctypes.POINTER(kvr_kv_cache)
+    lib.kvr_rotary_table.argtypes = [ctypes.POINTER(kvr_rope), I32, I64, P, P]
+    lib.kvr_rotary.argtypes = [P, P, I32, I64, I32, I32, I64, I64, I64, I64, P, P, I64, I32, I32,
+                               P, P]
+    lib.kvr_cache_write.argtypes = [C, P, P, I32, I64, I64, I64, I64, I64, P, P, P, I64, I32, I32,
+                                    P, P]
+    lib.kvr_cache_read.argtypes = [C, P, I64, P, P, I32, I64, I64, I64, I64, P, P]
+    lib.kvr_tree_attention.argtypes = [C, ctypes.POINTER(kvr_sequences), P, I32, I32, I64, I64, P,
+                                       I32, F, P, I64, I64, P, P, P,
+                                       ctypes.POINTER(ctypes.c_size_t), P]
+    for name in EXPORTS:
+        getattr(lib, name).restype = ctypes.c_int
+
+
+def _pkg():
+    import paper_2608_30830_amd as k
+    return k
+
+
+def _dtypes():
+    import torch
+    return {torch.bfloat16: KVR_DT_BF16, torch.float16: KVR_DT_FP16, torch.float32: KVR_DT_FP32}
+
+
+_DT = None
+
+
+def _dtype(t, name):
+    """The KVR_DT_* of a tensor."""
+    global _DT
+    if _DT is None:
+        _DT = _dtypes()
+    code = _DT.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be bfloat16, float16 or float32, not {t.dtype}")
+    return code
+
+
+def _rows(t, name, heads=None, dim=None, tokens=None):
+    """A [tokens, heads, dim] device tensor whose rows are adjacent elements."""
+    if not t.is_cuda or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1):
+        raise ValueError(f"{name} must be a [tokens, heads, dim] CUDA tensor with adjacent rows")
+    s = t.shape
+    if (tokens is not None and s[0] != tokens) or (heads is not None and s[1] != heads) or (
+            dim is not None and s[2] != dim):
+        raise ValueError(f"{name} must have shape {(tokens, heads, dim)}, not {tuple(s)}")
+    return t
+
+
+def _vector(t, dtype, count, name):
+    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or t.shape[0] != count or (
+            count > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous [{count}] {dtype} CUDA tensor")
+    return t
+
+
+def _finish(pkg, name, rc, check, status, stream, tensors):
+    """Raise on a host error; with check also wait for the device's."""
+    if rc:
+        pkg._check(rc, name)
+    if stream is not None:
+        pkg._on_stream(stream, *tensors)
+    if check:
+        torch = pkg._torch()
+        (torch.cuda.current_stream() if stream is None else stream).synchronize()
+        pkg._check(int(status.item()), f"{name}(device)")
+
+
+def _status(torch, check, status, stream):
+    """The status tensor of a call: the caller's, or with check a new one."""
+    if status is not None:
+        _vector(status, torch.int32, 1, "status")
+    elif check:
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        if stream is not None:   # zeroed on the current stream
+            stream.wait_stream(torch.cuda.current_stream())
+    return status
+
+
+class KvCache:
+    """The tensors of a paged cache, kept alive with the C view of them.
+
+    ``k``, ``v``: [n_pages, n_kv_heads, page_size, row], any strides with adjacent
+    rows (so permuted views of other orders too), the same for both.  bfloat16
+    or float16: row = head_dim elements.  uint8: codes, row = head_dim bytes (e4m3)
+    or head_dim / 2 (e2m1), with ``k_scale``, ``v_scale`` [n_pages, n_kv_heads,
+    page_size, head_dim / 32] uint8."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        import torch
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or v.stride() != k.stride():
+            raise ValueError("k and v must be [n_pages, n_kv_heads, page_size, row] alike")
+        if not k.is_cuda or not v.is_cuda or k.stride(3) != 1:
+            raise ValueError("k and v must be CUDA tensors with adjacent rows")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        pages, heads, page, row = k.shape
+        self.c = c = kvr_kv_cache()
+        if k.dtype == torch.uint8:
+            if k_scale is None or v_scale is None:
+                raise ValueError("a quantised cache needs k_scale and v_scale")
+            s = k_scale
+            if s.dim() != 4 or s.shape[:3] != k.shape[:3] or s.dtype != torch.uint8 or \
+                    not s.is_cuda or not v_scale.is_cuda or v_scale.shape != s.shape or \
+                    v_scale.dtype != s.dtype or v_scale.stride() != s.stride() or \
+                    (s.shape[3] > 1 and s.stride(3) != 1):
+                raise ValueError("k_scale and v_scale must be [n_pages, n_kv_heads, page_size, "
+                                 "head_dim / 32] uint8 CUDA tensors alike")
+            dim = BLOCK * s.shape[3]
+            if row not in (dim, dim // 2):
+                raise ValueError(f"rows of {row} bytes do not fit {s.shape[3]} scale bytes")
+            c.format = KVR_KV_FP8 if row == dim else KVR_KV_FP4
+            c.scale_page_stride, c.scale_head_stride, c.scale_token_stride = s.stride()[:3]
+            c.k_scale, c.v_scale = k_scale.data_ptr(), v_scale.data_ptr()
+        elif k.dtype in (torch.bfloat16, torch.float16):
+            if k_scale is not None or v_scale is not None:
+                raise ValueError("a 16-bit cache has no scales")
+            dim = row
+            c.format = KVR_KV_BF16 if k.dtype == torch.bfloat16 else KVR_KV_FP16
+        else:
+            raise ValueError(f"a cache holds bfloat16, float16 or uint8, not {k.dtype}")
+        e = k.element_size()
+        c.page_stride, c.head_stride, c.token_stride = (e * x for x in k.stride()[:3])
+        c.k_data, c.v_data = k.data_ptr(), v.data_ptr()
+        c.n_pages, c.page_size, c.n_kv_heads, c.head_dim = pages, page, heads, dim
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = pages, heads, page, dim
+        self.format = c.format
+        self.ref = ctypes.byref(c)
+
+    @classmethod
+    def allocate(cls, fmt: int, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int):
+        """An empty cache (zeros) on the current device."""
+        torch = _pkg()._torch()
+        lead = (n_pages, n_kv_heads, page_size)
+        if fmt in (KVR_KV_BF16, KVR_KV_FP16):
+            dt = torch.bfloat16 if fmt == KVR_KV_BF16 else torch.float16
+            return cls(*(torch.zeros(lead + (head_dim,), dtype=dt, device="cuda") for _ in "kv"))
+        if fmt not in (KVR_KV_FP8, KVR_KV_FP4):
+            raise ValueError(f"unknown cache format {fmt}")
+        row = head_dim if fmt == KVR_KV_FP8 else head_dim // 2
+        new = [torch.zeros(lead + (n,), dtype=torch.uint8, device="cuda")
+               for n in (row, row, head_dim // BLOCK, head_dim // BLOCK)]
+        return cls(*new)
+
+    @property
+    def tensors(self):
+        return self.k, self.v, self.k_scale, self.v_scale
+
+
+def kv_bytes_per_token(fmt: int, layers: int, n_kv_heads: int, head_dim: int) -> int:
+    """Bytes of one token's keys and values over all layers, scale bytes
+    included: the kv_bytes_per_token of kvr_prices_from_platform."""
+    row = {KVR_KV_BF16: 2 * head_dim, KVR_KV_FP16: 2 * head_dim,
+           KVR_KV_FP8: head_dim + head_dim // BLOCK,
+           KVR_KV_FP4: head_dim // 2 + head_dim // BLOCK}[fmt]
+    return 2 * layers * n_kv_heads * row
+
+
+def kvr_rotary_table(rot_dim: int, n_pos: int, theta: float = 10000.0,
+                     kind: int = KVR_ROPE_PLAIN, factor: float = 1.0, low: float = 1.0,
+                     high: float = 32.0, trained_len: float = 0.0, magnitude: float = 1.0,
+                     stream=None):
+    """cos and sin of every position and frequency, [n_pos, 2, rot_dim / 2] float32."""
+    k = _pkg()
+    torch = k._torch()
+    table = torch.empty((n_pos, 2, rot_dim // 2), dtype=torch.float32, device="cuda")
+    rope = kvr_rope(theta, factor, low, high, trained_len, magnitude, kind)
+    k._check(k.load_library().kvr_rotary_table(ctypes.byref(rope), rot_dim, n_pos,
+                                               table.data_ptr(), k._stream_ptr(stream)),
+             "kvr_rotary_table")
+    k._on_stream(stream, table)
+    return table
+
+
+def _table(torch, table, name="table"):
+    if not table.is_cuda or table.dtype != torch.float32 or table.dim() != 3 or \
+            table.shape[1] != 2 or not table.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [n_pos, 2, rot_dim / 2] float32 CUDA tensor")
+    return table.shape[0], 2 * table.shape[2]
+
+
+def _flags(interleaved, adjoint):
+    return (KVR_ROTARY_INTERLEAVED if interleaved else 0) | (KVR_ROTARY_ADJOINT if adjoint else 0)
+
+
+def kvr_rotary(x, positions, table, interleaved: bool = False, adjoint: bool = False, out=None,
+               status=None, stream=None, check: bool = True):
+    """x [tokens, heads, dim] turned by its positions; ``out`` may be ``x``."""
+    k = _pkg()
+    torch = k._torch()
+    _rows(x, "x")
+    dt = _dtype(x, "x")
+    n, h, d = x.shape
+    _vector(positions, torch.int32, n, "positions")
+    n_pos, rot = _table(torch, table)
+    if out is None:
+        out = torch.empty((n, h, d), dtype=x.dtype, device=x.device)
+    else:
+        _rows(out, "out", h, d, n)
+        if out.dtype != x.dtype:
+            raise ValueError("out must have the type of x")
+    status = _status(torch, check, status, stream)
+    xs, os_ = x.stride(), out.stride()
+    rc = k.load_library().kvr_rotary(
+        x.data_ptr(), out.data_ptr(), dt, n, h, d, xs[0], xs[1], os_[0], os_[1],
+        positions.data_ptr(), table.data_ptr(), n_pos, rot, _flags(interleaved, adjoint),
+        None if status is None else status.data_ptr(), k._stream_ptr(stream))
+    _finish(k, "kvr_rotary", rc, check, status, stream, (out, status))
+    return out
+
+
+def kvr_cache_write(cache: KvCache, k, v, slots, positions=None, table=None,
+                    interleaved: bool = False, adjoint: bool = False, status=None, stream=None,
+                    check: bool = True) -> None:
+    """k, v [tokens, n_kv_heads, head_dim] into ``slots`` [tokens] int64 (page *
+    page_size + row; below 0: not written); with ``table`` the keys are rotated by
+    ``positions`` on the way."""
+    p = _pkg()
+    torch = p._torch()
+    n = slots.shape[0]
+    _rows(k, "k", cache.n_kv_heads, cache.head_dim, n)
+    _rows(v, "v", cache.n_kv_heads, cache.head_dim, n)
+    dt = _dtype(k, "k")
+    if v.dtype != k.dtype:
+        raise ValueError("k and v must have one type")
+    _vector(slots, torch.int64, n, "slots")
+    n_pos = rot = 0
+    if table is not None:
+        n_pos, rot = _table(torch, table)
+        if positions is None:
+            raise ValueError("a table needs positions")
+        _vector(positions, torch.int32, n, "positions")
+    elif positions is not None:
+        raise ValueError("positions need a table")
+    status = _status(torch, check, status, stream)
+    ks, vs = k.stride(), v.stride()
+    rc = p.load_library().kvr_cache_write(
+        cache.ref, k.data_ptr(), v.data_ptr(), dt, n, ks[0], ks[1], vs[0], vs[1],
+        slots.data_ptr(), None if positions is None else positions.data_ptr(),
+        None if table is None else table.data_ptr(), n_pos, rot, _flags(interleaved, adjoint),
+        None if status is None else status.data_ptr(), p._stream_ptr(stream))
+    _finish(p, "kvr_cache_write", rc, check, status, stream, (status,))
+
+
+def kvr_cache_read(cache: KvCache, slots, dtype=None, out=None, status=None, stream=None,
+                   check: bool = True):
+    """(k, v) of ``slots`` [tokens] int64, each [tokens, n_kv_heads, head_dim] in
+    ``dtype`` (bfloat16 by default); below 0: zeros.  ``out``: a pair to write to."""
+    p = _pkg()
+    torch = p._torch()
+    n = slots.shape[0]
+    _vector(slots, torch.int64, n, "slots")
+    shape = (n, cache.n_kv_heads, cache.head_dim)
+    if out is None:
+        dtype = torch.bfloat16 if dtype is None else dtype
+        k, v = (torch.empty(shape, dtype=dtype, device=slots.device) for _ in "kv")
+    else:
+        k, v = out
+        _rows(k, "out k", shape[1], shape[2], n)
+        _rows(v, "out v", shape[1], shape[2], n)
+        if v.dtype != k.dtype or (dtype is not None and k.dtype != dtype):
+            raise ValueError("out must be two tensors of the type that is asked for")
+    dt = _dtype(k, "out")
+    status = _status(torch, check, status, stream)
+    ks, vs = k.stride(), v.stride()
+    rc = p.load_library().kvr_cache_read(
+        cache.ref, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(), dt, ks[0], ks[1], vs[0], vs[1],
+        None if status is None else status.data_ptr(), p._stream_ptr(stream))
+    _finish(p, "kvr_cache_read", rc, check, status, stream, (k, v, status))
+    return k, v
+
+
+def kvr_tree_attention(cache: KvCache, q, cu_q, kv_len, page_table, max_q: int, max_kv: int,
+                       tree_mask=None, scale: Optional[float] = None, want_lse: bool = False,
+                       out=None, workspace=None, status=None, stream=None, check: bool = True):
+    """Attention of each sequence's newest tokens over its pages of the cache.
+
+    ``q`` [n_queries, n_q_heads, head_dim]; ``cu_q`` [n_seqs + 1] and ``kv_len``
+    [n_seqs] int32; ``page_table`` [n_seqs, pages] int32; ``max_q``, ``max_kv``: bounds
+    on a sequence's new and cached tokens; ``tree_mask`` [n_queries, words] int64
+    (bit j: newest token j is seen) or None (the newest tokens up to itself);
+    ``scale`` defaults to head_dim ** -0.5.  Returns out, or (out, lse
+    [n_queries, n_q_heads] float32) with ``want_lse``."""
+    p = _pkg()
+    torch = p._torch()
+    _rows(q, "q", None, cache.head_dim)
+    dt = _dtype(q, "q")
+    n, h, d = q.shape
+    seqs = kv_len.shape[0]
+    _vector(kv_len, torch.int32, seqs, "kv_len")
+    _vector(cu_q, torch.int32, seqs + 1, "cu_q")
+    if not page_table.is_cuda or page_table.dtype != torch.int32 or page_table.dim() != 2 or \
+            page_table.shape[0] != seqs or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table must be a [n_seqs, pages] int32 CUDA tensor")
+    words = 0
+    if tree_mask is not None:
+        if not tree_mask.is_cuda or tree_mask.dtype != torch.int64 or tree_mask.dim() != 2 or \
+                tree_mask.shape[0] != n or not tree_mask.is_contiguous():
+            raise ValueError("tree_mask must be a contiguous [n_queries, words] int64 CUDA tensor")
+        words = tree_mask.shape[1]
+    if out is None:
+        out = torch.empty((n, h, d), dtype=q.dtype, device=q.device)
+    else:
+        _rows(out, "out", h, d, n)
+        if out.dtype != q.dtype:
+            raise ValueError("out must have the type of q")
+    lse = torch.empty((n, h), dtype=torch.float32, device=q.device) if want_lse else None
+    s = kvr_sequences(cu_q.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
+                      page_table.stride(0), page_table.shape[1], n, seqs, max_q, max_kv)
+    status = _status(torch, check, status, stream)
+    lib = p.load_library()
+    qs, os_ = q.stride(), out.stride()
+    need = ctypes.c_size_t(0)
+    mask_ptr = None if tree_mask is None else tree_mask.data_ptr()
+    sc = 1.0 / math.sqrt(d) if scale is None else scale
+
+    def call(ws):
+        return lib.kvr_tree_attention(
+            cache.ref, s, q.data_ptr(), dt, h, qs[0], qs[1], mask_ptr, words, sc, out.data_ptr(),
+            os_[0], os_[1], None if lse is None else lse.data_ptr(),
+            None if status is None else status.data_ptr(), ws, need, p._stream_ptr(stream))
+
+    rc = call(None)
+    if rc:
+        p._check(rc, "kvr_tree_attention(size)")
+    ws = p._workspace(need.value, workspace)
+    need.value = ws.numel()
+    rc = call(ws.data_ptr())
+    _finish(p, "kvr_tree_attention", rc, check, status, stream, (out, lse, ws, status))
+    return (out, lse) if want_lse else out

@@ -33,32 +33,29 @@ namespace kvr {
 namespace kv {
 namespace {
 
-// Every wave computes the same: the parts of all sequences, and where `item` falls.
+// Where `item` falls: parts of sequences in order, each part's row blocks next to each
+// other.  Every wave computes the same.
 __device__ Part find_part(const Attention &a, int item)
 {
     const int lane = threadIdx.x & 63;
-    int64_t total = 0;
-    for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
-        int len = 0, nq = 0, q0;
-        if (b0 + lane < a.n_seqs) sequence(a, b0 + lane, len, nq, q0);
-        total += wave_sum(steps_of(len, nq));
-    }
-    const int per = part_steps(a, total);
+    const int per = part_steps(a);
     int base = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
         int len = 0, nq = 0, q0 = 0;
         if (b0 + lane < a.n_seqs) sequence(a, b0 + lane, len, nq, q0);
-        const int steps = steps_of(len, nq);
+        const int steps = steps_of(len, nq), rbs = row_blocks_of(a, nq);
         const int parts = (steps + per - 1) / per;
-        const int upto = wave_scan(parts);
+        const int upto = wave_scan(parts * rbs);
         const uint64_t hit = __ballot(base + upto > item);
         if (hit) {
             const int w = __ffsll((unsigned long long)hit) - 1;
             Part p;
             p.b = b0 + w;
             p.parts = lane_value(parts, w);
-            p.base = base + lane_value(upto, w) - p.parts;
-            p.part = item - p.base;
+            const int nrb = lane_value(rbs, w);
+            const int at = item - (base + lane_value(upto, w) - p.parts * nrb);
+            p.part = at / nrb;
+            p.rb = at - p.part * nrb;
             p.len = lane_value(len, w);
             p.nq = lane_value(nq, w);
             p.q0 = lane_value(q0, w);
@@ -199,31 +196,42 @@ __device__ __forceinline__ uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel)
     return __builtin_amdgcn_perm(hi, lo, sel);
 }
 
-template <int FMT, int QT, int NB, int RT, int PF>
+template <int FMT, int QT, int NB, int RT, int PF, bool Shared>
 struct Kernel {
     static constexpr int D = NB * 32;
     static constexpr bool Quant = Fmt<FMT>::Quant;
     static constexpr int MT = FMT == KVR_KV_FP16 ? KVR_DT_FP16 : KVR_DT_BF16;   // product type
-    // a half-precision query against a quantised cache is split into two bfloat16 parts
+    // Half-precision queries and weights meet a quantised cache as two bfloat16 parts.
     static constexpr int QS = Quant && QT == KVR_DT_FP16 ? 2 : 1;
-    static constexpr int Rows16 = 16 * RT;
+    static constexpr int BlockRows = (Shared ? kWaves : 1) * 16 * RT;
     static constexpr int LdsRow = D + 4;
     using KR = KeyRaw<FMT, NB>;
     using VR = ValRaw<FMT, NB>;
 
-    struct Stage {
+    struct Stage {   // one step as loaded
         KR k[2];
         VR v;
     };
+    struct State {   // of this wave's rows
+        u32x4 q[RT][QS][NB];
+        f32x4 o[RT][2 * NB];
+        float m[RT], l[RT];   // reference maximum (log2), this lane's part of the sum
+        int qi[RT];           // query within the sequence
+    };
+    // LDS: the joining of the waves (maxima, sums, values), or one step of each wave in
+    // the order that the matrix instructions read: keys [2][NB][64], values [2 NB][64].
+    static constexpr int JoinWords = 2 * kWaves * BlockRows + BlockRows * LdsRow;
+    static constexpr int StepWords = 4 * NB * 64 * 4;
+    static constexpr int LdsWords = Shared ? kWaves * StepWords : JoinWords;
 
     const Attention &a;
-    const uint32_t n, g;
-    int h, len, prefix;
+    const uint32_t n, g, lane;
+    int h, len, prefix, q0;
     const int32_t *pages;
     uint32_t krow, vrow, ksrow, vsrow;   // byte offsets of this lane's rows in a tile
 
     __device__ Kernel(const Attention &a_)
-        : a(a_), n(threadIdx.x & 15), g((threadIdx.x & 63) >> 4)
+        : a(a_), n(threadIdx.x & 15), g((threadIdx.x & 63) >> 4), lane(threadIdx.x & 63)
     {
         krow = (uint32_t)n * (uint32_t)a.c.token_stride;
         vrow = 4u * (uint32_t)g * (uint32_t)a.c.token_stride;
@@ -324,202 +332,288 @@ struct Kernel {
         }
     }
 
-    __device__ __forceinline__ static bool nonfinite(uint32_t x)
+    // Infinities and NaN among a lane's loaded values, and those values to zero.
+    static constexpr uint32_t kExp = FMT == KVR_KV_FP16 ? 0x7c00u : 0x7f80u;
+    __device__ __forceinline__ static bool odd_values(const VR &v)
     {
-        constexpr uint32_t e = MT == KVR_DT_BF16 ? 0x7f80u : 0x7c00u;
-        return (x & e) == e || (x & (e << 16)) == (e << 16);
-    }
-
-    // Non-finite halves of x to zero, and what they were: 1 (NaN), 64 (+inf) or 4096 (-inf).
-    __device__ __forceinline__ static void split(uint32_t &x, uint32_t &flag)
-    {
-        constexpr uint32_t e = MT == KVR_DT_BF16 ? 0x7f80u : 0x7c00u;
-        flag = 0;
-        uint32_t kept = 0;
+        bool odd = false;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t y = (x >> (16 * i)) & 0xffffu;
-            float f = 0.0f;
-            if ((y & e) == e) f = (y & 0x7fffu) != e ? 1.0f : (y & 0x8000u) ? 4096.0f : 64.0f;
-            else kept |= y << (16 * i);
-            flag |= (pack16<MT>(f, 0.0f) & 0xffffu) << (16 * i);
+        for (int t = 0; t < 8; ++t) {
+#pragma unroll
+            for (int w = 0; w < VR::words; ++w) {
+                const uint32_t x = v.w[t][w];
+                if (!Quant) odd = odd || (x & kExp) == kExp || (x & kExp << 16) == kExp << 16;
+                if (FMT == KVR_KV_FP8)   // a byte of 0x7f or 0xff: its low seven bits + 1 carry
+                    odd = odd || (((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+            }
+            if (Quant)
+#pragma unroll
+                for (int s = 0; s < VR::slabs; ++s) odd = odd || v.s[t][s] == kBadScale;
         }
-        x = kept;
+        return __ballot(odd) != 0;
+    }
+    __device__ __forceinline__ static void clear_odd(VR &v)
+    {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+#pragma unroll
+            for (int w = 0; w < VR::words; ++w) {
+                uint32_t x = v.w[t][w];
+                if (!Quant) {
+                    if ((x & kExp) == kExp) x &= 0xffff0000u;
+                    if ((x & kExp << 16) == kExp << 16) x &= 0xffffu;
+                }
+                if (FMT == KVR_KV_FP8)
+                    x &= ~(((((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 255u);
+                v.w[t][w] = x;
+            }
+            if (Quant)
+#pragma unroll
+                for (int s = 0; s < VR::slabs; ++s)
+                    if (v.s[t][s] == kBadScale) {   // the block's words may be shared: codes to zero
+                        v.s[t][s] = 127;
+#pragma unroll
+                        for (int w = VR::word(s); w < VR::word(s + 1); ++w) v.w[t][w] = 0;
+                    }
+        }
     }
 
-    // One step: scores of 32 tokens, softmax update, values.
-    __device__ __forceinline__ void compute(int step, Stage &st, const u32x4 (&q)[RT][QS][NB],
-                                            f32x4 (&o)[RT][2 * NB], float (&m)[RT], float (&l)[RT],
-                                            const int (&qi)[RT], int q0, int nq) const
+    // Token i (of this lane's eight) of a step.
+    __device__ __forceinline__ int token(int step, int i) const
     {
-        const int t0 = step * kStep;
+        return step * kStep + 16 * (i >> 2) + 4 * (int)g + (i & 3);
+    }
+
+    // Rows past the sequence's end hold anything: they read as zeros.
+    __device__ __forceinline__ void clear_past_end(int step, VR &v) const
+    {
+        if ((step + 1) * kStep <= len) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (token(step, i) >= len) {
+#pragma unroll
+                for (int w = 0; w < VR::words; ++w) v.w[i][w] = 0;
+                if (Quant)
+#pragma unroll
+                    for (int s = 0; s < VR::slabs; ++s) v.s[i][s] = 127;
+            }
+    }
+
+    // A step's values as the products may take them: rows past the end as zeros, and where
+    // tokens are hidden from some rows, infinities and NaN as zeros too (a weight of
+    // zero would not hide them); add_odd puts them back for the rows that see them.
+    __device__ __forceinline__ bool clean(int step, VR &v) const
+    {
+        if ((step + 1) * kStep <= prefix) return false;   // nothing is hidden
+        clear_past_end(step, v);
+        const bool odd = odd_values(v);
+        if (odd) clear_odd(v);
+        return odd;
+    }
+
+    // Element d of token t's value, if it is an infinity or a NaN, else 0.
+    __device__ __forceinline__ float odd_at(int t, int d) const
+    {
+        int id = pages[t >> a.c.page_shift];
+        if (id < 0 || id >= a.c.n_pages) id = 0;
+        const int off = t & ((1 << a.c.page_shift) - 1);
+        const char *row = a.c.v + id * a.c.page_stride + h * a.c.head_stride + off * a.c.token_stride;
+        if (!Quant) {
+            const uint16_t x = reinterpret_cast<const uint16_t *>(row)[d];
+            if ((x & kExp) != kExp) return 0.0f;
+            return load1<FMT == KVR_KV_FP16 ? KVR_DT_FP16 : KVR_DT_BF16>(row, d);
+        }
+        bool nan = a.c.vs[id * a.c.spage_stride + h * a.c.shead_stride + off * a.c.stoken_stride +
+                          (d >> 5)] == kBadScale;
+        if (FMT == KVR_KV_FP8)
+            nan = nan || (reinterpret_cast<const uint8_t *>(row)[d] & 0x7f) == 0x7f;
+        return nan ? __uint_as_float(0x7fc00000u) : 0.0f;
+    }
+    // The infinities and NaN that clean() took out, to W elements of one row.
+    template <int W>
+    __device__ __forceinline__ void add_odd(const Part &p, int row, int d, float *x) const
+    {
+        const int i = row / a.group;
+        const int t1 = min(len, p.last * kStep);
+        for (int t = max(p.first, prefix / kStep) * kStep; t < t1; ++t) {
+            if (!sees(i, t - prefix)) continue;
+#pragma unroll
+            for (int e = 0; e < W; ++e) {
+                const float y = odd_at(t, d + e);
+                if (y != 0.0f) x[e] += y;   // NaN included
+            }
+        }
+    }
+    // Whether query i sees newest token j (older ones: j < 0).
+    __device__ __forceinline__ bool sees(int i, int j) const
+    {
+        if (j < 0) return true;
+        if (a.mask) return (a.mask[(int64_t)(q0 + i) * a.words + (j >> 6)] >> (j & 63)) & 1;
+        return j <= i;
+    }
+
+    // Value tiles 2 I and 2 I + 1 of a step: element pairs of eight tokens turned around.
+    template <int I>
+    __device__ __forceinline__ void val_tiles(const VR &v, u32x4 (&x)[2]) const
+    {
+        uint32_t c[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) c[t] = val_pair<I>(v, t);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            x[0][t] = perm(c[2 * t + 1], c[2 * t], 0x05040100u);
+            x[1][t] = perm(c[2 * t + 1], c[2 * t], 0x07060302u);
+        }
+    }
+
+    // Softmax of one row tile's scores of a step: the weights in the products' type
+    // and the rescaled state.  The reference maximum moves only
+    // when a score exceeds it by more than 8 (a factor of 2^8, which costs the
+    // weights no precision), so most steps need no exchange between lanes.
+    __device__ __forceinline__ void weights(int step, int r, const f32x4 (&sc)[2], State &st,
+                                            u32x4 (&pv)[QS]) const
+    {
+        float x[8];
+        uint32_t seen = 0xff;
+        const bool masked = (step + 1) * kStep > prefix;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = sc[i >> 2][i & 3];
+        if (masked) {
+            seen = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int t = token(step, i);
+                const bool v = t < len && sees(st.qi[r], t - prefix);
+                x[i] = v ? x[i] : -INFINITY;
+                seen |= (v ? 1u : 0u) << i;
+            }
+        }
+        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+                          fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        top = top == -INFINITY ? kLowest : top * a.scale2;
+        if (__ballot(top > st.m[r] + 8.0f)) {
+            top = fmaxf(row_max(top), st.m[r]);
+            const float f = __builtin_amdgcn_exp2f(st.m[r] - top);
+            st.l[r] *= f;
+#pragma unroll
+            for (int e = 0; e < 2 * NB; ++e) st.o[r][e] *= f;
+            st.m[r] = top;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(x[i], a.scale2, -st.m[r]);
+        if (masked) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = seen >> i & 1 ? x[i] : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
+        st.l[r] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            pv[0][i] = pack16<MT>(x[2 * i], x[2 * i + 1]);
+            if (QS == 2) {
+                float y0, y1;
+                unpack16<MT>(pv[0][i], y0, y1);
+                pv[QS - 1][i] = pack16<MT>(x[2 * i] - y0, x[2 * i + 1] - y1);
+            }
+        }
+    }
+
+    // O^T += V^T P^T of one value tile.
+    __device__ __forceinline__ void accumulate(int e, u32x4 x, const u32x4 (&pv)[RT][QS],
+                                               State &st) const
+    {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int p = 0; p < QS; ++p) st.o[r][e] = mfma<MT>(x, pv[r][p], st.o[r][e]);
+    }
+
+    // One step from registers; returns whether values were taken out.
+    __device__ __forceinline__ bool compute(int step, Stage &raw, State &st) const
+    {
         f32x4 sc[RT][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
             for (int r = 0; r < RT; ++r) sc[r][t] = f32x4{0, 0, 0, 0};
             static_for<0, NB>([&](auto I) {
-                constexpr int i = decltype(I)::value;
-                const u32x4 kb = key_block<i>(st.k[t]);
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int p = 0; p < QS; ++p) sc[r][t] = mfma<MT>(kb, q[r][p][i], sc[r][t]);
+                const u32x4 kb = key_block<decltype(I)::value>(raw.k[t]);
+                scores(decltype(I)::value, t, kb, st, sc);
             });
         }
-        const bool masked = t0 + kStep > prefix;
-        const bool ends = t0 + kStep > len;
-        u32x4 pv[RT], vis[RT];
+        u32x4 pv[RT][QS];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            float x[8];
-            uint32_t seen = 0xff;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = sc[r][i >> 2][i & 3] * a.scale2;
-            if (masked) {
-                seen = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int t = t0 + 16 * (i >> 2) + 4 * (int)g + (i & 3);
-                    const int j = t - prefix;
-                    bool v = j < 0;
-                    if (!v && t < len) {
-                        if (a.mask)
-                            v = (a.mask[(int64_t)(q0 + qi[r]) * a.words + (j >> 6)] >> (j & 63)) & 1;
-                        else v = j <= qi[r];
-                    }
-                    x[i] = v ? x[i] : -INFINITY;
-                    seen |= (v ? 1u : 0u) << i;
-                }
-            }
-            float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
-                              fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            top = fmaxf(row_max(top), m[r]);
-            if (__ballot(top > m[r])) {
-                const float f = __builtin_amdgcn_exp2f(m[r] - top);
-                l[r] *= f;
-#pragma unroll
-                for (int e = 0; e < 2 * NB; ++e) o[r][e] *= f;
-                m[r] = top;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] = __builtin_amdgcn_exp2f(x[i] - m[r]);
-                l[r] += x[i];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                pv[r][i] = pack16<MT>(x[2 * i], x[2 * i + 1]);
-                vis[r][i] = masked ? pack16<MT>(seen >> (2 * i) & 1, seen >> (2 * i + 1) & 1) : 0u;
-            }
-        }
-        if (ends) {   // rows past the end hold anything: they read as zeros
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (t0 + 16 * (i >> 2) + 4 * (int)g + (i & 3) >= len) {
-#pragma unroll
-                    for (int w = 0; w < VR::words; ++w) st.v.w[i][w] = 0;
-                    if (Quant)
-#pragma unroll
-                        for (int s = 0; s < VR::slabs; ++s) st.v.s[i][s] = 127;
-                }
-        }
-        bool odd = false;
-        if (masked) {   // may a hidden token hold an infinity or a NaN?
-            static_for<0, NB>([&](auto I) {
-#pragma unroll
-                for (int t = 0; t < 8; ++t) odd = odd || nonfinite(val_pair<decltype(I)::value>(st.v, t));
-            });
-        }
-        if (__ballot(odd)) values<true>(st.v, pv, vis, o);
-        else values<false>(st.v, pv, vis, o);
-    }
-
-    // O^T += V^T P^T.  Odd: the non-finite values are taken out and counted apart, for
-    // the rows that see their tokens.
-    template <bool Odd>
-    __device__ __forceinline__ void values(const VR &v, const u32x4 (&pv)[RT], const u32x4 (&vis)[RT],
-                                           f32x4 (&o)[RT][2 * NB]) const
-    {
+        for (int r = 0; r < RT; ++r) weights(step, r, sc[r], st, pv[r]);
+        const bool odd = clean(step, raw.v);
         static_for<0, NB>([&](auto I) {
-            constexpr int i = decltype(I)::value;   // elements 2 i and 2 i + 1 of the chunks
-            uint32_t c[8];
-#pragma unroll
-            for (int t = 0; t < 8; ++t) c[t] = val_pair<i>(v, t);
             u32x4 x[2];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                x[0][t] = perm(c[2 * t + 1], c[2 * t], 0x05040100u);
-                x[1][t] = perm(c[2 * t + 1], c[2 * t], 0x07060302u);
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                u32x4 flags;
-                if (Odd) {
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        uint32_t y = x[e][t], f;
-                        split(y, f);
-                        x[e][t] = y;
-                        flags[t] = f;
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    if (Odd) {
-                        const f32x4 f = mfma<MT>(flags, vis[r], f32x4{0, 0, 0, 0});
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int bits = (int)f[k];
-                            float add = 0.0f;
-                            if ((bits & 63) || ((bits & 4032) && bits >= 4096))
-                                add = __uint_as_float(0x7fc00000u);
-                            else if (bits >= 4096) add = -INFINITY;
-                            else if (bits) add = INFINITY;
-                            o[r][2 * i + e][k] += add;
-                        }
-                    }
-                    o[r][2 * i + e] = mfma<MT>(x[e], pv[r], o[r][2 * i + e]);
-                }
-            }
+            val_tiles<decltype(I)::value>(raw.v, x);
+            accumulate(2 * decltype(I)::value, x[0], pv, st);
+            accumulate(2 * decltype(I)::value + 1, x[1], pv, st);
         });
+        return odd;
+    }
+    __device__ __forceinline__ void scores(int i, int t, u32x4 kb, const State &st,
+                                           f32x4 (&sc)[RT][2]) const
+    {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int p = 0; p < QS; ++p) sc[r][t] = mfma<MT>(kb, st.q[r][p][i], sc[r][t]);
     }
 
-    __device__ __forceinline__ void run(float *lds)
+    // A step into LDS, converted and turned around, and from there.
+    __device__ __forceinline__ bool put(int step, Stage &raw, uint32_t *lds) const
     {
-        // The row blocks of one part share its cached tokens: they go to one XCD
-        // (block number mod 8), one after another.
-        const int rb8 = 8 * a.row_blocks;
-        const int grp = blockIdx.x / rb8, in = blockIdx.x - grp * rb8;
-        const int rb = in >> 3;
-        const int unit = grp * 8 + (in & 7);
-        const int nh = a.c.n_heads;
-        const int item = unit / nh;
-        h = unit - item * nh;
-        const Part p = find_part(a, item);
-        if (p.b < 0) return;
-        const int rows = p.nq * a.group;
-        const int r0 = rb * Rows16;
-        if (r0 >= rows) return;
-        len = p.len;
-        prefix = p.len - p.nq;
-        pages = a.pages + (int64_t)p.b * a.pages_stride;
+        u32x4 *kf = reinterpret_cast<u32x4 *>(lds) + lane, *vf = kf + 2 * NB * 64;
+        const bool odd = clean(step, raw.v);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            static_for<0, NB>([&](auto I) {
+                kf[(t * NB + decltype(I)::value) * 64] = key_block<decltype(I)::value>(raw.k[t]);
+            });
+        static_for<0, NB>([&](auto I) {
+            u32x4 x[2];
+            val_tiles<decltype(I)::value>(raw.v, x);
+            vf[(2 * decltype(I)::value) * 64] = x[0];
+            vf[(2 * decltype(I)::value + 1) * 64] = x[1];
+        });
+        return odd;
+    }
+    __device__ __forceinline__ void compute_shared(int step, const uint32_t *lds, State &st) const
+    {
+        const u32x4 *kf = reinterpret_cast<const u32x4 *>(lds) + lane, *vf = kf + 2 * NB * 64;
+        f32x4 sc[RT][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) sc[r][t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < NB; ++i) scores(i, t, kf[(t * NB + i) * 64], st, sc);
+        }
+        u32x4 pv[RT][QS];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) weights(step, r, sc[r], st, pv[r]);
+#pragma unroll
+        for (int e = 0; e < 2 * NB; ++e) accumulate(e, vf[e * 64], pv, st);
+    }
 
-        u32x4 q[RT][QS][NB];
-        f32x4 o[RT][2 * NB];
-        float m[RT], l[RT];
-        int qi[RT];
+    // Queries of the 16-row tiles from row r0 on; rows past the last repeat it.
+    __device__ __forceinline__ void load_queries(int r0, int rows, State &st) const
+    {
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            const int row = min(r0 + 16 * r + (int)n, rows - 1);   // rows past the last repeat it
-            qi[r] = row / a.group;
-            const int head = h * a.group + (row - qi[r] * a.group);
-            const char *src = a.q.p + ((int64_t)(p.q0 + qi[r]) * a.q.token_stride +
+            const int row = min(r0 + 16 * r + (int)n, rows - 1);
+            st.qi[r] = row / a.group;
+            const int head = h * a.group + (row - st.qi[r] * a.group);
+            const char *src = a.q.p + ((int64_t)(q0 + st.qi[r]) * a.q.token_stride +
                                        (int64_t)head * a.q.head_stride) * 2;
+            const uint32_t flip = a.negate ? 0x80008000u : 0u;
             static_for<0, NB>([&](auto I) {
                 constexpr int i = decltype(I)::value, s = KR::slab_of(i), start = KR::start(s);
                 const int d = start * 32 + g * KR::width(s) * 8 + (i - start) * 8;
-                u32x4 x = *reinterpret_cast<const u32x4 *>(src + d * 2);
+                u32x4 x = *reinterpret_cast<const u32x4 *>(src + d * 2) ^ flip;
                 if (QS == 2) {
                     u32x4 lo;
 #pragma unroll
@@ -530,135 +624,230 @@ struct Kernel {
                         unpack16<KVR_DT_BF16>(x[t], y0, y1);
                         lo[t] = pack_bf16(x0 - y0, x1 - y1);
                     }
-                    q[r][QS - 1][i] = lo;
+                    st.q[r][QS - 1][i] = lo;
                 }
-                q[r][0][i] = x;
+                st.q[r][0][i] = x;
             });
-            m[r] = kLowest;
-            l[r] = 0.0f;
+            st.m[r] = kLowest;
+            st.l[r] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 2 * NB; ++e) o[r][e] = f32x4{0, 0, 0, 0};
+            for (int e = 0; e < 2 * NB; ++e) st.o[r][e] = f32x4{0, 0, 0, 0};
         }
+    }
 
+    // W adjacent elements (2, 4 or 8) of a row of the output, or of a part's.
+    template <int W>
+    __device__ __forceinline__ void store(const Part &p, int64_t cell, int r0, int row, int d,
+                                          const float *x, float top, float sum) const
+    {
+        if (p.parts != 1) {
+            float *y = a.part_o + (cell * BlockRows + row) * D + d;
+#pragma unroll
+            for (int e = 0; e < W; ++e) y[e] = x[e];
+            if (d == 0) {
+                a.part_ml[(cell * BlockRows + row) * 2] = top;
+                a.part_ml[(cell * BlockRows + row) * 2 + 1] = sum;
+            }
+            return;
+        }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const int i0 = (r0 + row) / a.group;
+        const int head = h * a.group + (r0 + row - i0 * a.group);
+        uint32_t *y = reinterpret_cast<uint32_t *>(
+            a.out.p + ((int64_t)(q0 + i0) * a.out.token_stride + (int64_t)head * a.out.head_stride + d) * 2);
+        uint32_t w[W / 2];
+#pragma unroll
+        for (int e = 0; e < W / 2; ++e) w[e] = pack16<QT>(x[2 * e] * inv, x[2 * e + 1] * inv);
+        if constexpr (W == 8) *reinterpret_cast<u32x4 *>(y) = u32x4{w[0], w[1], w[2], w[3]};
+        else if constexpr (W == 4) *reinterpret_cast<u32x2 *>(y) = u32x2{w[0], w[1]};
+        else *y = w[0];
+        if (d == 0 && a.lse)
+            a.lse[(int64_t)(q0 + i0) * a.q_heads + head] =
+                sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+
+    __device__ __forceinline__ void run(uint32_t *lds)
+    {
+        // Heads fastest: with eight or a multiple of them the row blocks of one part, which
+        // follow each other, land on one XCD (block number mod 8) and share its L2.
+        const int item = blockIdx.x / a.c.n_heads;
+        h = blockIdx.x - item * a.c.n_heads;
+        const Part p = find_part(a, item);
+        if (p.b < 0) return;
+        const int rows = p.nq * a.group, r0 = p.rb * BlockRows;
+        len = p.len;
+        prefix = p.len - p.nq;
+        q0 = p.q0;
+        pages = a.pages + (int64_t)p.b * a.pages_stride;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        Stage st[PF];
+        if constexpr (Shared) run_shared(p, wave, r0, rows, lds);
+        else run_split(p, wave, r0, rows, reinterpret_cast<float *>(lds));
+    }
+
+    // Few rows: every wave has all of the block's rows and every n-th step.
+    __device__ __forceinline__ void run_split(const Part &p, int wave, int r0, int rows, float *lds)
+    {
+        State st;
+        Stage raw[PF];
+        bool odd = false;
         int s = p.first + wave;
 #pragma unroll
         for (int i = 0; i < PF; ++i)
-            if (s + i * kWaves < p.last) load(s + i * kWaves, st[i]);
+            if (s + i * kWaves < p.last) load(s + i * kWaves, raw[i]);
+        load_queries(r0, rows, st);
         for (; s < p.last; s += PF * kWaves) {
 #pragma unroll
             for (int i = 0; i < PF; ++i) {
                 const int at = s + i * kWaves;
                 if (at < p.last) {
-                    compute(at, st[i], q, o, m, l, qi, p.q0, p.nq);
-                    if (at + PF * kWaves < p.last) load(at + PF * kWaves, st[i]);
+                    odd |= compute(at, raw[i], st);
+                    if (at + PF * kWaves < p.last) load(at + PF * kWaves, raw[i]);
                 }
             }
         }
-
         // join the waves: maxima first, then sums and values in wave order
-        float *sm = lds, *sl = lds + kWaves * Rows16, *so = lds + 2 * kWaves * Rows16;
+        float *sm = lds, *sl = lds + kWaves * BlockRows, *so = lds + 2 * kWaves * BlockRows;
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            l[r] = row_sum(l[r]);
+            st.l[r] = row_sum(st.l[r]);
             if (g == 0) {
-                sm[wave * Rows16 + 16 * r + n] = m[r];
-                sl[wave * Rows16 + 16 * r + n] = l[r];
+                sm[wave * BlockRows + 16 * r + n] = st.m[r];
+                sl[wave * BlockRows + 16 * r + n] = st.l[r];
             }
         }
-        __syncthreads();
+        odd = __syncthreads_or(odd);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             float top = kLowest;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm[w * Rows16 + 16 * r + n]);
-            const float f = __builtin_amdgcn_exp2f(m[r] - top);
+            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm[w * BlockRows + 16 * r + n]);
+            const float f = __builtin_amdgcn_exp2f(st.m[r] - top);
 #pragma unroll
-            for (int e = 0; e < 2 * NB; ++e) o[r][e] *= f;
+            for (int e = 0; e < 2 * NB; ++e) st.o[r][e] *= f;
         }
         for (int w = 0; w < kWaves; ++w) {
             if (wave == w) {
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
                     float *row = so + (16 * r + n) * LdsRow;
-static_for<0, 2 * NB>([&](auto E) {
+                    static_for<0, 2 * NB>([&](auto E) {
                         // tile e of its slab: element (4 g + i) * W + e - e0 of the slab
                         constexpr int e = decltype(E)::value, slab = VR::slab_of(e);
                         constexpr int e0 = VR::first(slab), W = VR::width(slab);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             float *x = row + 16 * e0 + (4 * g + i) * W + (e - e0);
-                            *x = w == 0 ? o[r][e][i] : *x + o[r][e][i];
+                            *x = w == 0 ? st.o[r][e][i] : *x + st.o[r][e][i];
                         }
                     });
                 }
             }
             __syncthreads();
         }
-
         // rows out: eight elements a thread
-        const bool whole = p.parts == 1;
-        const int64_t cell = ((int64_t)(p.base + p.part) * nh + h) * a.row_blocks + rb;
-        for (int i = threadIdx.x; i < Rows16 * (D / 8); i += kThreads) {
+        const int64_t cell = blockIdx.x;
+        for (int i = threadIdx.x; i < BlockRows * (D / 8); i += kThreads) {
             const int row = i / (D / 8), d = 8 * (i - row * (D / 8));
             if (r0 + row >= rows) break;
             float top = kLowest, sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm[w * Rows16 + row]);
+            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm[w * BlockRows + row]);
 #pragma unroll
             for (int w = 0; w < kWaves; ++w)
-                sum += sl[w * Rows16 + row] * __builtin_amdgcn_exp2f(sm[w * Rows16 + row] - top);
+                sum += sl[w * BlockRows + row] * __builtin_amdgcn_exp2f(sm[w * BlockRows + row] - top);
             float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = so[row * LdsRow + d + e];
-            if (!whole) {
-                store8<KVR_DT_FP32>(
-                    reinterpret_cast<char *>(a.part_o + (cell * Rows16 + row) * D + d), x);
-                if (d == 0) {
-                    a.part_ml[(cell * Rows16 + row) * 2] = top;
-                    a.part_ml[(cell * Rows16 + row) * 2 + 1] = sum;
-                }
-                continue;
+            if (odd) add_odd<8>(p, r0 + row, d, x);
+            store<8>(p, cell, r0, row, d, x, top, sum);
+        }
+    }
+
+    // Many rows: the waves divide the block's rows; each brings one step of a group of
+    // four into LDS, and all of them work on all four.
+    __device__ __forceinline__ void run_shared(const Part &p, int wave, int r0, int rows, uint32_t *lds)
+    {
+        const int w0 = 16 * RT * wave;
+        const bool active = r0 + w0 < rows;
+        State st;
+        Stage raw;
+        if (p.first + wave < p.last) load(p.first + wave, raw);
+        load_queries(r0 + w0, rows, st);
+        bool odd = false;
+        for (int s = p.first; s < p.last; s += kWaves) {
+            if (s + wave < p.last) {
+                odd |= put(s + wave, raw, lds + wave * StepWords);
+                if (s + kWaves + wave < p.last) load(s + kWaves + wave, raw);
             }
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            __syncthreads();
+            if (active) {
+                const int count = min(kWaves, p.last - s);
+                for (int u = 0; u < count; ++u) compute_shared(s + u, lds + u * StepWords, st);
+            }
+            __syncthreads();
+        }
+        odd = __syncthreads_or(odd);
+        const int64_t cell = blockIdx.x;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] *= inv;
-            const int i0 = (r0 + row) / a.group;
-            const int head = h * a.group + (r0 + row - i0 * a.group);
-            store8<QT>(a.out.p + ((int64_t)(p.q0 + i0) * a.out.token_stride +
-                                  (int64_t)head * a.out.head_stride + d) * 2, x);
-            if (d == 0 && a.lse)
-                a.lse[(int64_t)(p.q0 + i0) * a.q_heads + head] =
-                    sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        for (int r = 0; r < RT; ++r) {
+            const int row = w0 + 16 * r + (int)n;
+            const float sum = row_sum(st.l[r]);
+            if (r0 + row >= rows) continue;
+            static_for<0, VR::slabs>([&](auto S) {
+                constexpr int e0 = VR::first(decltype(S)::value), W = VR::width(decltype(S)::value);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x[W];
+#pragma unroll
+                    for (int e = 0; e < W; ++e) x[e] = st.o[r][e0 + e][i];
+                    const int d = 16 * e0 + (4 * (int)g + i) * W;
+                    if (odd) add_odd<W>(p, r0 + row, d, x);
+                    store<W>(p, cell, r0, row, d, x, st.m[r], sum);
+                }
+            });
         }
     }
 };
 
-template <int FMT, int QT, int NB, int RT, int PF>
-__global__ __launch_bounds__(kThreads, 2) void attention_kernel(Attention a)
+// Waves per SIMD that the registers are bounded for: two, or one where a wave's
+// accumulators, queries and rows in flight need more than 256.
+template <int NB, int RT>
+constexpr int waves_per_simd()
 {
-    __shared__ float lds[2 * kWaves * 16 * RT + 16 * RT * (NB * 32 + 4)];
-    Kernel<FMT, QT, NB, RT, PF> k(a);
+    return NB * RT > 8 ? 1 : 2;
+}
+
+template <int FMT, int QT, int NB, int RT, int PF, bool Shared>
+__global__ __launch_bounds__(kThreads, (waves_per_simd<NB, RT>())) void attention_kernel(Attention a)
+{
+    using K = Kernel<FMT, QT, NB, RT, PF, Shared>;
+    __shared__ __align__(16) uint32_t lds[K::LdsWords];
+    K k(a);
     k.run(lds);
 }
 
 // One launch for a format and query type, the head size and the row tiles chosen here.
 template <int FMT, int QT, int NB, int RT>
-hipError_t launch_rt(const Attention &a, dim3 grid, hipStream_t stream)
+hipError_t launch_split(const Attention &a, dim3 grid, hipStream_t stream)
 {
     constexpr int stage = NB * Fmt<FMT>::B8;   // registers of one step's keys and values
-    constexpr int room = (Fmt<FMT>::Quant ? 64 : RT == 1 ? 128 : 64) / stage;
+    constexpr int room = (RT == 2 ? (Fmt<FMT>::Quant ? 32 : 64) : Fmt<FMT>::Quant ? 64 : 128) / stage;
     constexpr int PF = room < 1 ? 1 : room > 3 ? 3 : room;
-    attention_kernel<FMT, QT, NB, RT, PF><<<grid, kThreads, 0, stream>>>(a);
+    attention_kernel<FMT, QT, NB, RT, PF, false><<<grid, kThreads, 0, stream>>>(a);
     return hipGetLastError();
 }
 
 template <int FMT, int QT, int NB>
 hipError_t launch_nb(const Attention &a, dim3 grid, hipStream_t stream)
 {
-    if (a.row_tiles == 1) return launch_rt<FMT, QT, NB, 1>(a, grid, stream);
-    return launch_rt<FMT, QT, NB, 2>(a, grid, stream);
+    if (a.shared) {
+        if (a.row_tiles == 1)
+            attention_kernel<FMT, QT, NB, 1, 1, true><<<grid, kThreads, 0, stream>>>(a);
+        else attention_kernel<FMT, QT, NB, 2, 1, true><<<grid, kThreads, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+    if (a.row_tiles == 1) return launch_split<FMT, QT, NB, 1>(a, grid, stream);
+    return launch_split<FMT, QT, NB, 2>(a, grid, stream);
 }
 
 template <int FMT, int QT>

@@ -8,82 +8,89 @@ namespace kvr {
 namespace kv {
 namespace {
 
-// Joins the parts of one row: dim / 4 lanes x groups of parts, each group over its
-// share of the parts, then the groups in order.
-template <int QT>
-__global__ __launch_bounds__(256) void combine_kernel(Attention a, int dim)
+// Joins the parts of rows.  A row has dim / 4 lanes times Groups groups of parts: each
+// group sums its share of the parts, then the groups are added in order.  With many
+// rows one group does, with few eight keep more loads in flight.
+template <int QT, int Groups>
+__global__ __launch_bounds__(256) void combine_kernel(Attention a)
 {
-    __shared__ float so[1024];   // [groups][dim]
-    __shared__ float sl[32];
-    const int nh = a.c.n_heads;
-    const int rows16 = 16 * a.row_tiles;
-    // block: (query row slot, head, sequence)
-    const int row = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+    __shared__ float so[Groups > 1 ? 1024 : 1];
+    __shared__ float sl[Groups > 1 ? 256 : 1];
+    const int dim = a.c.dim, cols = dim / 4;
+    const int per_row = cols * Groups;
+    const int rows_per_block = 256 / per_row;
+    const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63;
     int len, nq, q0;
     sequence(a, b, len, nq, q0);
-    if (row >= nq * a.group) return;
-    // this sequence's parts
-    const int lane = threadIdx.x & 63;
-    int64_t total = 0;
-    for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
-        int le = 0, nn = 0, qq;
-        if (b0 + lane < a.n_seqs) sequence(a, b0 + lane, le, nn, qq);
-        total += wave_sum(steps_of(le, nn));
-    }
-    const int per = part_steps(a, total);
+    const int rows = nq * a.group;
+    if ((int)blockIdx.x * rows_per_block >= rows) return;
+    const int per = part_steps(a);
     const int parts = (steps_of(len, nq) + per - 1) / per;
     if (parts <= 1) return;
-    int base = 0;
+    int base = 0;   // items before this sequence's
     for (int b0 = 0; b0 < b; b0 += 64) {
         int le = 0, nn = 0, qq;
         if (b0 + lane < b) sequence(a, b0 + lane, le, nn, qq);
-        base += wave_sum((steps_of(le, nn) + per - 1) / per);
+        base += wave_sum((steps_of(le, nn) + per - 1) / per * row_blocks_of(a, nn));
     }
-    const int rb = row / rows16, rr = row - rb * rows16;
+    const int local = threadIdx.x / per_row, rest = threadIdx.x - local * per_row;
+    const int grp = rest / cols, c = rest - grp * cols;
+    const int row = blockIdx.x * rows_per_block + local;
+    const bool live = local < rows_per_block && row < rows;
+    const int rb = row / a.block_rows, rr = row - rb * a.block_rows;
+    const int nrb = row_blocks_of(a, nq);
     auto cell = [&](int p) {
-        return (((int64_t)(base + p) * nh + h) * a.row_blocks + rb) * rows16 + rr;
+        return ((int64_t)(base + p * nrb + rb) * a.c.n_heads + h) * a.block_rows + rr;
     };
-    float top = kLowest;
-    for (int p = lane; p < parts; p += 64) top = fmaxf(top, a.part_ml[2 * cell(p)]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const int cols = dim / 4;                 // 8 to 64 lanes of four elements
-    const int groups = 256 / cols;
-    const int grp = threadIdx.x / cols, c = threadIdx.x - grp * cols;
     f32x4 acc = {0, 0, 0, 0};
-    float sum = 0.0f;
-    if (grp < groups) {
+    float sum = 0.0f, top = kLowest;
+    if (live) {
+        for (int p = 0; p < parts; ++p) top = fmaxf(top, a.part_ml[2 * cell(p)]);
 #pragma unroll 4
-        for (int p = grp; p < parts; p += groups) {
+        for (int p = grp; p < parts; p += Groups) {
             const int64_t at = cell(p);
             const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * at] - top);
             sum += f * a.part_ml[2 * at + 1];
             acc += f * *reinterpret_cast<const f32x4 *>(a.part_o + at * dim + 4 * c);
         }
-        *reinterpret_cast<f32x4 *>(so + grp * dim + 4 * c) = acc;
-        if (c == 0) sl[grp] = sum;
     }
-    __syncthreads();
-    const int tid = threadIdx.x;
-    if (tid < dim / 8) {
-        float x[8] = {};
-        float s = 0.0f;
-        for (int p = 0; p < groups; ++p) {
-            s += sl[p];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] += so[p * dim + 8 * tid + e];
+    if constexpr (Groups > 1) {
+        if (live) {
+            *reinterpret_cast<f32x4 *>(so + 4 * threadIdx.x) = acc;
+            sl[threadIdx.x] = sum;
         }
-        const float inv = s == 0.0f ? 0.0f : 1.0f / s;
+        __syncthreads();
+        if (!live || grp != 0) return;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] *= inv;
-        const int i0 = row / a.group;
-        const int head = h * a.group + (row - i0 * a.group);
-        store8<QT>(a.out.p + ((int64_t)(q0 + i0) * a.out.token_stride +
-                              (int64_t)head * a.out.head_stride + 8 * tid) * 2, x);
-        if (tid == 0 && a.lse)
-            a.lse[(int64_t)(q0 + i0) * a.q_heads + head] =
-                s == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(s)) * kLn2;
+        for (int p = 1; p < Groups; ++p) {
+            const int t = threadIdx.x + p * cols;
+            acc += *reinterpret_cast<const f32x4 *>(so + 4 * t);
+            sum += sl[t];
+        }
     }
+    if (!live) return;
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int i0 = row / a.group;
+    const int head = h * a.group + (row - i0 * a.group);
+    uint32_t *y = reinterpret_cast<uint32_t *>(
+        a.out.p + ((int64_t)(q0 + i0) * a.out.token_stride + (int64_t)head * a.out.head_stride + 4 * c) * 2);
+    *reinterpret_cast<u32x2 *>(y) = u32x2{pack16<QT>(acc[0] * inv, acc[1] * inv),
+                                          pack16<QT>(acc[2] * inv, acc[3] * inv)};
+    if (c == 0 && a.lse)
+        a.lse[(int64_t)(q0 + i0) * a.q_heads + head] =
+            sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+template <int QT>
+hipError_t launch_combine(const Attention &a, hipStream_t stream)
+{
+    const int64_t rows = (int64_t)a.max_q * a.group;
+    const int groups = rows * a.c.n_heads * a.n_seqs >= 4096 || a.c.dim > 128 ? 1 : 8;
+    const int per_block = 256 / (a.c.dim / 4 * groups);
+    const dim3 grid((unsigned)cdiv(rows, std::max(1, per_block)), a.c.n_heads, a.n_seqs);
+    if (groups == 1) combine_kernel<QT, 1><<<grid, 256, 0, stream>>>(a);
+    else combine_kernel<QT, 8><<<grid, 256, 0, stream>>>(a);
+    return hipGetLastError();
 }
 
 constexpr int kSlots = 1024;   // blocks that the parts are planned for
@@ -93,24 +100,25 @@ constexpr int kSlots = 1024;   // blocks that the parts are planned for
 size_t plan_attention(Attention &a)
 {
     const int64_t rows = (int64_t)a.max_q * a.group;
-    a.row_tiles = rows <= 16 ? 1 : 2;
-    a.row_blocks = (int32_t)cdiv(rows, 16 * a.row_tiles);
-    a.target = (int32_t)std::max<int64_t>(1, kSlots / ((int64_t)a.c.n_heads * a.row_blocks));
+    a.shared = rows > 32;
+    a.row_tiles = rows <= 16 || (rows > 32 && rows <= 64) ? 1 : 2;
+    a.block_rows = 16 * a.row_tiles * (a.shared ? kWaves : 1);
+    a.target = std::max(1, kSlots / a.c.n_heads);
     a.min_steps = 4 * kWaves;
     const int64_t longest = cdiv(a.max_kv, kStep);
-    // ceil per sequence of at least min_steps, and about target in all
-    const int64_t bound = std::min<int64_t>((int64_t)a.target + a.n_seqs,
-                                            a.n_seqs * cdiv(longest, a.min_steps));
-    a.max_parts = (int32_t)std::max<int64_t>(1, bound);
+    // Row blocks of all sequences; ceil(steps / part) parts of each, part = total / target
+    // or min_steps.
+    const int64_t blocks = std::min<int64_t>((int64_t)a.n_seqs * cdiv(rows, a.block_rows),
+                                             a.n_queries * a.group / a.block_rows + a.n_seqs);
+    a.max_items = (int32_t)std::max<int64_t>(
+        1, std::min(a.target + blocks, blocks * cdiv(longest, a.min_steps)));
     if (longest <= a.min_steps) return 0;
-    return (size_t)a.max_parts * a.c.n_heads * a.row_blocks * 16 * a.row_tiles *
-           (a.c.dim + 2) * sizeof(float);
+    return (size_t)a.max_items * a.c.n_heads * a.block_rows * (a.c.dim + 2) * sizeof(float);
 }
 
 hipError_t launch_attention(const Attention &a, hipStream_t stream)
 {
-    const int64_t units = cdiv((int64_t)a.max_parts * a.c.n_heads, 8) * 8;
-    const dim3 grid((unsigned)(units * a.row_blocks));
+    const dim3 grid((unsigned)((int64_t)a.max_items * a.c.n_heads));
     const bool half = a.q.dtype == KVR_DT_FP16;
     hipError_t e;
     switch (a.c.format) {
@@ -123,10 +131,7 @@ hipError_t launch_attention(const Attention &a, hipStream_t stream)
         e = half ? launch_attention_fp4h(a, grid, stream) : launch_attention_fp4(a, grid, stream);
     }
     if (e != hipSuccess || a.part_o == nullptr) return e;
-    const dim3 joins((unsigned)(a.max_q * a.group), a.c.n_heads, a.n_seqs);
-    if (half) combine_kernel<KVR_DT_FP16><<<joins, 256, 0, stream>>>(a, a.c.dim);
-    else combine_kernel<KVR_DT_BF16><<<joins, 256, 0, stream>>>(a, a.c.dim);
-    return hipGetLastError();
+    return half ? launch_combine<KVR_DT_FP16>(a, stream) : launch_combine<KVR_DT_BF16>(a, stream);
 }
 
 }  // namespace kv

@@ -71,15 +71,17 @@ struct Attention {
     const uint64_t *mask;        // [n_queries][words] or nullptr (each token sees the ones before it)
     int64_t n_queries, pages_stride, max_pages;
     int32_t n_seqs, q_heads, group, max_q, max_kv, words;
-    float scale2;                // softmax scale * log2(e)
+    float scale2;                // |softmax scale| * log2(e)
+    int32_t negate;              // the scale is negative: queries change sign
     // launch plan
-    int32_t row_tiles;           // 16-row tiles of one block
-    int32_t row_blocks;          // blocks that cover max_q * group rows
-    int32_t target;              // parts that all sequences together are cut into, about
-    int32_t max_parts;           // bound on the parts
+    int32_t row_tiles;           // 16-row tiles of one wave
+    int32_t shared;              // waves share cached tokens and divide rows (else the reverse)
+    int32_t block_rows;          // rows of one block
+    int32_t target;              // items (a part of a sequence x a block of rows) of one head, about
+    int32_t max_items;           // bound on them
     int32_t min_steps;           // steps that a part has at least
-    float *part_o;               // [parts][heads][row_blocks][16 * row_tiles][dim]
-    float *part_ml;              // [parts][heads][row_blocks][16 * row_tiles][2]
+    float *part_o;               // [items][heads][block_rows][dim]
+    float *part_ml;              // [items][heads][block_rows][2]
     int *status;
 };
 

@@ -249,6 +249,7 @@ int kvr_tree_attention(const kvr_kv_cache *cache, const kvr_sequences *seqs, con
     a.n_seqs = seqs->n_seqs;
     a.max_q = seqs->max_q;
     a.max_kv = seqs->max_kv;
+    a.n_queries = seqs->n_queries;
     const size_t need = kvr::kv::plan_attention(a);
     if (!d_ws) {
         *ws_bytes = need;
@@ -266,10 +267,10 @@ int kvr_tree_attention(const kvr_kv_cache *cache, const kvr_sequences *seqs, con
     a.pages = seqs->d_pages;
     a.pages_stride = seqs->pages_stride;
     a.max_pages = seqs->max_pages;
-    a.n_queries = seqs->n_queries;
     a.mask = d_tree_mask;
     a.words = mask_words;
-    a.scale2 = (float)((double)scale * 1.4426950408889634);
+    a.scale2 = (float)(std::fabs((double)scale) * 1.4426950408889634);
+    a.negate = scale < 0.0f;
     a.status = d_status;
     if (need) {
         const size_t cells = need / sizeof(float) / (size_t)(a.c.dim + 2);

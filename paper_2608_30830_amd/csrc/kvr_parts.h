@@ -18,8 +18,8 @@ constexpr float kLowest = -3.402823466e38f;
 struct Part {
     int b;            // sequence; -1: nothing to do
     int part, parts;  // which of how many
+    int rb;           // block of rows
     int first, last;  // steps [first, last)
-    int base;         // parts before this sequence's
     int len, nq, q0;  // cached tokens, new tokens, first query
 };
 
@@ -63,10 +63,24 @@ __device__ __forceinline__ int steps_of(int len, int nq)
 {
     return nq > 0 ? (len + kStep - 1) / kStep : 0;
 }
-
-// Steps of one part: all sequences' steps over the target, at least min_steps.
-__device__ __forceinline__ int part_steps(const Attention &a, int64_t total)
+__device__ __forceinline__ int row_blocks_of(const Attention &a, int nq)
 {
+    return (nq * a.group + a.block_rows - 1) / a.block_rows;
+}
+
+// Steps of one part: all sequences' steps (times their row blocks) over the
+// target, at least min_steps.
+__device__ __forceinline__ int part_steps(const Attention &a)
+{
+    const int lane = threadIdx.x & 63;
+    int64_t total = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
+        int len = 0, nq = 0, q0;
+        if (b0 + lane < a.n_seqs) sequence(a, b0 + lane, len, nq, q0);
+        // at most 2^26 steps x 2^20 row blocks of 64 sequences: summed in two halves
+        const int64_t w = (int64_t)steps_of(len, nq) * row_blocks_of(a, nq);
+        total += (int64_t)wave_sum((int)(w & 0xffffff)) + ((int64_t)wave_sum((int)(w >> 24)) << 24);
+    }
     const int64_t n = (total + a.target - 1) / a.target;
     return (int)(n > a.min_steps ? n : a.min_steps);
 }

@@ -75,69 +75,83 @@ def declare(lib) -> None:
         getattr(lib, name).restype = ctypes.c_int
 
 
-def _pkg():
-    import paper_2608_30830_amd as k
-    return k
+class _Context:
+    """torch, the package and the loaded library, looked up once."""
+
+    def __init__(self):
+        import torch
+        import paper_2608_30830_amd as pkg
+        pkg._torch()   # raises without a GPU
+        self.torch, self.pkg, self.lib = torch, pkg, pkg.load_library()
+        self.codes = {torch.bfloat16: KVR_DT_BF16, torch.float16: KVR_DT_FP16,
+                      torch.float32: KVR_DT_FP32}
+        # the current stream's handle without making a Stream object (2.7 us less a call)
+        self.raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+    def stream(self, stream, device):
+        if stream is not None:
+            return stream.cuda_stream
+        if self.raw is not None:
+            return self.raw(device.index)
+        return self.torch.cuda.current_stream(device).cuda_stream
 
 
-def _dtypes():
-    import torch
-    return {torch.bfloat16: KVR_DT_BF16, torch.float16: KVR_DT_FP16, torch.float32: KVR_DT_FP32}
+_CTX: Optional[_Context] = None
 
 
-_DT = None
+def _context() -> _Context:
+    global _CTX
+    if _CTX is None:
+        _CTX = _Context()
+    return _CTX
 
 
-def _dtype(t, name):
+def _dtype(x, t, name):
     """The KVR_DT_* of a tensor."""
-    global _DT
-    if _DT is None:
-        _DT = _dtypes()
-    code = _DT.get(t.dtype)
+    code = x.codes.get(t.dtype)
     if code is None:
         raise ValueError(f"{name} must be bfloat16, float16 or float32, not {t.dtype}")
     return code
 
 
 def _rows(t, name, heads=None, dim=None, tokens=None):
-    """A [tokens, heads, dim] device tensor whose rows are adjacent elements."""
-    if not t.is_cuda or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1):
+    """Shape and strides of a [tokens, heads, dim] device tensor with adjacent rows."""
+    shape, stride = t.shape, t.stride()
+    if not t.is_cuda or len(shape) != 3 or (stride[2] != 1 and shape[2] != 1):
         raise ValueError(f"{name} must be a [tokens, heads, dim] CUDA tensor with adjacent rows")
-    s = t.shape
-    if (tokens is not None and s[0] != tokens) or (heads is not None and s[1] != heads) or (
-            dim is not None and s[2] != dim):
-        raise ValueError(f"{name} must have shape {(tokens, heads, dim)}, not {tuple(s)}")
-    return t
+    if (tokens is not None and shape[0] != tokens) or (heads is not None and shape[1] != heads) or (
+            dim is not None and shape[2] != dim):
+        raise ValueError(f"{name} must have shape {(tokens, heads, dim)}, not {tuple(shape)}")
+    return shape, stride
 
 
 def _vector(t, dtype, count, name):
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 1 or t.shape[0] != count or (
-            count > 1 and t.stride(0) != 1):
+    """Address of a contiguous [count] device tensor."""
+    if not t.is_cuda or t.dtype != dtype or t.shape != (count,) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous [{count}] {dtype} CUDA tensor")
-    return t
+    return t.data_ptr()
 
 
-def _finish(pkg, name, rc, check, status, stream, tensors):
-    """Raise on a host error; with check also wait for the device's."""
-    if rc:
-        pkg._check(rc, name)
-    if stream is not None:
-        pkg._on_stream(stream, *tensors)
-    if check:
-        torch = pkg._torch()
-        (torch.cuda.current_stream() if stream is None else stream).synchronize()
-        pkg._check(int(status.item()), f"{name}(device)")
-
-
-def _status(torch, check, status, stream):
+def _status(x, check, status, stream):
     """The status tensor of a call: the caller's, or with check a new one."""
     if status is not None:
-        _vector(status, torch.int32, 1, "status")
+        _vector(status, x.torch.int32, 1, "status")
     elif check:
-        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        status = x.torch.zeros(1, dtype=x.torch.int32, device="cuda")
         if stream is not None:   # zeroed on the current stream
-            stream.wait_stream(torch.cuda.current_stream())
+            stream.wait_stream(x.torch.cuda.current_stream())
     return status
+
+
+def _finish(x, name, rc, check, status, stream, *tensors):
+    """Raise on a host error; with check also wait for the device's."""
+    if rc:
+        x.pkg._check(rc, name)
+    if stream is not None:
+        x.pkg._on_stream(stream, status, *tensors)
+    if check:
+        (x.torch.cuda.current_stream() if stream is None else stream).synchronize()
+        x.pkg._check(int(status.item()), f"{name}(device)")
 
 
 class KvCache:
@@ -192,7 +206,7 @@ class KvCache:
     @classmethod
     def allocate(cls, fmt: int, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int):
         """An empty cache (zeros) on the current device."""
-        torch = _pkg()._torch()
+        torch = _context().torch
         lead = (n_pages, n_kv_heads, page_size)
         if fmt in (KVR_KV_BF16, KVR_KV_FP16):
             dt = torch.bfloat16 if fmt == KVR_KV_BF16 else torch.float16
@@ -223,22 +237,22 @@ def kvr_rotary_table(rot_dim: int, n_pos: int, theta: float = 10000.0,
                      high: float = 32.0, trained_len: float = 0.0, magnitude: float = 1.0,
                      stream=None):
     """cos and sin of every position and frequency, [n_pos, 2, rot_dim / 2] float32."""
-    k = _pkg()
-    torch = k._torch()
-    table = torch.empty((n_pos, 2, rot_dim // 2), dtype=torch.float32, device="cuda")
+    x = _context()
+    table = x.torch.empty((n_pos, 2, rot_dim // 2), dtype=x.torch.float32, device="cuda")
     rope = kvr_rope(theta, factor, low, high, trained_len, magnitude, kind)
-    k._check(k.load_library().kvr_rotary_table(ctypes.byref(rope), rot_dim, n_pos,
-                                               table.data_ptr(), k._stream_ptr(stream)),
-             "kvr_rotary_table")
-    k._on_stream(stream, table)
+    rc = x.lib.kvr_rotary_table(ctypes.byref(rope), rot_dim, n_pos, table.data_ptr(),
+                                x.stream(stream, table.device))
+    _finish(x, "kvr_rotary_table", rc, False, None, stream, table)
     return table
 
 
-def _table(torch, table, name="table"):
-    if not table.is_cuda or table.dtype != torch.float32 or table.dim() != 3 or \
-            table.shape[1] != 2 or not table.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous [n_pos, 2, rot_dim / 2] float32 CUDA tensor")
-    return table.shape[0], 2 * table.shape[2]
+def _table(x, table):
+    """Address, positions and rotated elements of a rotary table."""
+    shape = table.shape
+    if not table.is_cuda or table.dtype != x.torch.float32 or len(shape) != 3 or shape[1] != 2 or \
+            not table.is_contiguous():
+        raise ValueError("table must be a contiguous [n_pos, 2, rot_dim / 2] float32 CUDA tensor")
+    return table.data_ptr(), shape[0], 2 * shape[2]
 
 
 def _flags(interleaved, adjoint):
@@ -248,26 +262,25 @@ def _flags(interleaved, adjoint):
 def kvr_rotary(x, positions, table, interleaved: bool = False, adjoint: bool = False, out=None,
                status=None, stream=None, check: bool = True):
     """x [tokens, heads, dim] turned by its positions; ``out`` may be ``x``."""
-    k = _pkg()
-    torch = k._torch()
-    _rows(x, "x")
-    dt = _dtype(x, "x")
-    n, h, d = x.shape
-    _vector(positions, torch.int32, n, "positions")
-    n_pos, rot = _table(torch, table)
+    c = _context()
+    (n, h, d), xs = _rows(x, "x")
+    dt = _dtype(c, x, "x")
+    pos = _vector(positions, c.torch.int32, n, "positions")
+    t, n_pos, rot = _table(c, table)
     if out is None:
-        out = torch.empty((n, h, d), dtype=x.dtype, device=x.device)
+        out = c.torch.empty((n, h, d), dtype=x.dtype, device=x.device)
+        o0, o1 = h * d, d
     else:
-        _rows(out, "out", h, d, n)
+        _, (o0, o1, _) = _rows(out, "out", h, d, n)
         if out.dtype != x.dtype:
             raise ValueError("out must have the type of x")
-    status = _status(torch, check, status, stream)
-    xs, os_ = x.stride(), out.stride()
-    rc = k.load_library().kvr_rotary(
-        x.data_ptr(), out.data_ptr(), dt, n, h, d, xs[0], xs[1], os_[0], os_[1],
-        positions.data_ptr(), table.data_ptr(), n_pos, rot, _flags(interleaved, adjoint),
-        None if status is None else status.data_ptr(), k._stream_ptr(stream))
-    _finish(k, "kvr_rotary", rc, check, status, stream, (out, status))
+    if check or status is not None:
+        status = _status(c, check, status, stream)
+    rc = c.lib.kvr_rotary(x.data_ptr(), out.data_ptr(), dt, n, h, d, xs[0], xs[1], o0, o1, pos, t,
+                          n_pos, rot, _flags(interleaved, adjoint),
+                          None if status is None else status.data_ptr(), c.stream(stream, x.device))
+    if rc or check or stream is not None:
+        _finish(c, "kvr_rotary", rc, check, status, stream, out)
     return out
 
 
@@ -277,58 +290,59 @@ def kvr_cache_write(cache: KvCache, k, v, slots, positions=None, table=None,
     """k, v [tokens, n_kv_heads, head_dim] into ``slots`` [tokens] int64 (page *
     page_size + row; below 0: not written); with ``table`` the keys are rotated by
     ``positions`` on the way."""
-    p = _pkg()
-    torch = p._torch()
+    c = _context()
     n = slots.shape[0]
-    _rows(k, "k", cache.n_kv_heads, cache.head_dim, n)
-    _rows(v, "v", cache.n_kv_heads, cache.head_dim, n)
-    dt = _dtype(k, "k")
+    _, ks = _rows(k, "k", cache.n_kv_heads, cache.head_dim, n)
+    _, vs = _rows(v, "v", cache.n_kv_heads, cache.head_dim, n)
+    dt = _dtype(c, k, "k")
     if v.dtype != k.dtype:
         raise ValueError("k and v must have one type")
-    _vector(slots, torch.int64, n, "slots")
+    at = _vector(slots, c.torch.int64, n, "slots")
+    pos = t = None
     n_pos = rot = 0
     if table is not None:
-        n_pos, rot = _table(torch, table)
+        t, n_pos, rot = _table(c, table)
         if positions is None:
             raise ValueError("a table needs positions")
-        _vector(positions, torch.int32, n, "positions")
+        pos = _vector(positions, c.torch.int32, n, "positions")
     elif positions is not None:
         raise ValueError("positions need a table")
-    status = _status(torch, check, status, stream)
-    ks, vs = k.stride(), v.stride()
-    rc = p.load_library().kvr_cache_write(
-        cache.ref, k.data_ptr(), v.data_ptr(), dt, n, ks[0], ks[1], vs[0], vs[1],
-        slots.data_ptr(), None if positions is None else positions.data_ptr(),
-        None if table is None else table.data_ptr(), n_pos, rot, _flags(interleaved, adjoint),
-        None if status is None else status.data_ptr(), p._stream_ptr(stream))
-    _finish(p, "kvr_cache_write", rc, check, status, stream, (status,))
+    if check or status is not None:
+        status = _status(c, check, status, stream)
+    rc = c.lib.kvr_cache_write(cache.ref, k.data_ptr(), v.data_ptr(), dt, n, ks[0], ks[1], vs[0],
+                               vs[1], at, pos, t, n_pos, rot, _flags(interleaved, adjoint),
+                               None if status is None else status.data_ptr(),
+                               c.stream(stream, slots.device))
+    if rc or check or stream is not None:
+        _finish(c, "kvr_cache_write", rc, check, status, stream)
 
 
 def kvr_cache_read(cache: KvCache, slots, dtype=None, out=None, status=None, stream=None,
                    check: bool = True):
     """(k, v) of ``slots`` [tokens] int64, each [tokens, n_kv_heads, head_dim] in
     ``dtype`` (bfloat16 by default); below 0: zeros.  ``out``: a pair to write to."""
-    p = _pkg()
-    torch = p._torch()
+    c = _context()
     n = slots.shape[0]
-    _vector(slots, torch.int64, n, "slots")
-    shape = (n, cache.n_kv_heads, cache.head_dim)
+    at = _vector(slots, c.torch.int64, n, "slots")
+    heads, dim = cache.n_kv_heads, cache.head_dim
     if out is None:
-        dtype = torch.bfloat16 if dtype is None else dtype
-        k, v = (torch.empty(shape, dtype=dtype, device=slots.device) for _ in "kv")
+        dtype = c.torch.bfloat16 if dtype is None else dtype
+        k, v = c.torch.empty((2, n, heads, dim), dtype=dtype, device=slots.device)
+        ks = vs = (heads * dim, dim)
     else:
         k, v = out
-        _rows(k, "out k", shape[1], shape[2], n)
-        _rows(v, "out v", shape[1], shape[2], n)
+        _, ks = _rows(k, "out k", heads, dim, n)
+        _, vs = _rows(v, "out v", heads, dim, n)
         if v.dtype != k.dtype or (dtype is not None and k.dtype != dtype):
             raise ValueError("out must be two tensors of the type that is asked for")
-    dt = _dtype(k, "out")
-    status = _status(torch, check, status, stream)
-    ks, vs = k.stride(), v.stride()
-    rc = p.load_library().kvr_cache_read(
-        cache.ref, slots.data_ptr(), n, k.data_ptr(), v.data_ptr(), dt, ks[0], ks[1], vs[0], vs[1],
-        None if status is None else status.data_ptr(), p._stream_ptr(stream))
-    _finish(p, "kvr_cache_read", rc, check, status, stream, (k, v, status))
+    dt = _dtype(c, k, "out")
+    if check or status is not None:
+        status = _status(c, check, status, stream)
+    rc = c.lib.kvr_cache_read(cache.ref, at, n, k.data_ptr(), v.data_ptr(), dt, ks[0], ks[1], vs[0],
+                              vs[1], None if status is None else status.data_ptr(),
+                              c.stream(stream, slots.device))
+    if rc or check or stream is not None:
+        _finish(c, "kvr_cache_read", rc, check, status, stream, k, v)
     return k, v
 
 
@@ -343,50 +357,49 @@ def kvr_tree_attention(cache: KvCache, q, cu_q, kv_len, page_table, max_q: int, 
     (bit j: newest token j is seen) or None (the newest tokens up to itself);
     ``scale`` defaults to head_dim ** -0.5.  Returns out, or (out, lse
     [n_queries, n_q_heads] float32) with ``want_lse``."""
-    p = _pkg()
-    torch = p._torch()
-    _rows(q, "q", None, cache.head_dim)
-    dt = _dtype(q, "q")
-    n, h, d = q.shape
+    c = _context()
+    torch = c.torch
+    (n, h, d), qs = _rows(q, "q", None, cache.head_dim)
+    dt = _dtype(c, q, "q")
     seqs = kv_len.shape[0]
-    _vector(kv_len, torch.int32, seqs, "kv_len")
-    _vector(cu_q, torch.int32, seqs + 1, "cu_q")
-    if not page_table.is_cuda or page_table.dtype != torch.int32 or page_table.dim() != 2 or \
-            page_table.shape[0] != seqs or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+    lens = _vector(kv_len, torch.int32, seqs, "kv_len")
+    cu = _vector(cu_q, torch.int32, seqs + 1, "cu_q")
+    shape, stride = page_table.shape, page_table.stride()
+    if not page_table.is_cuda or page_table.dtype != torch.int32 or len(shape) != 2 or \
+            shape[0] != seqs or (shape[1] > 1 and stride[1] != 1):
         raise ValueError("page_table must be a [n_seqs, pages] int32 CUDA tensor")
-    words = 0
+    mask, words = None, 0
     if tree_mask is not None:
         if not tree_mask.is_cuda or tree_mask.dtype != torch.int64 or tree_mask.dim() != 2 or \
                 tree_mask.shape[0] != n or not tree_mask.is_contiguous():
             raise ValueError("tree_mask must be a contiguous [n_queries, words] int64 CUDA tensor")
-        words = tree_mask.shape[1]
+        mask, words = tree_mask.data_ptr(), tree_mask.shape[1]
     if out is None:
         out = torch.empty((n, h, d), dtype=q.dtype, device=q.device)
+        o0, o1 = h * d, d
     else:
-        _rows(out, "out", h, d, n)
+        _, (o0, o1, _) = _rows(out, "out", h, d, n)
         if out.dtype != q.dtype:
             raise ValueError("out must have the type of q")
     lse = torch.empty((n, h), dtype=torch.float32, device=q.device) if want_lse else None
-    s = kvr_sequences(cu_q.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(),
-                      page_table.stride(0), page_table.shape[1], n, seqs, max_q, max_kv)
-    status = _status(torch, check, status, stream)
-    lib = p.load_library()
-    qs, os_ = q.stride(), out.stride()
-    need = ctypes.c_size_t(0)
-    mask_ptr = None if tree_mask is None else tree_mask.data_ptr()
-    sc = 1.0 / math.sqrt(d) if scale is None else scale
-
-    def call(ws):
-        return lib.kvr_tree_attention(
-            cache.ref, s, q.data_ptr(), dt, h, qs[0], qs[1], mask_ptr, words, sc, out.data_ptr(),
-            os_[0], os_[1], None if lse is None else lse.data_ptr(),
-            None if status is None else status.data_ptr(), ws, need, p._stream_ptr(stream))
-
-    rc = call(None)
+    if check or status is not None:
+        status = _status(c, check, status, stream)
+    s = kvr_sequences(cu, lens, page_table.data_ptr(), stride[0], shape[1], n, seqs, max_q, max_kv)
+    nbytes = ctypes.c_size_t(0)
+    call = c.lib.kvr_tree_attention
+    args = (cache.ref, s, q.data_ptr(), dt, h, qs[0], qs[1], mask, words,
+            1.0 / math.sqrt(d) if scale is None else scale, out.data_ptr(), o0, o1,
+            None if lse is None else lse.data_ptr(), None if status is None else status.data_ptr())
+    rc = call(*args, None, nbytes, None)
     if rc:
-        p._check(rc, "kvr_tree_attention(size)")
-    ws = p._workspace(need.value, workspace)
-    need.value = ws.numel()
-    rc = call(ws.data_ptr())
-    _finish(p, "kvr_tree_attention", rc, check, status, stream, (out, lse, ws, status))
+        c.pkg._check(rc, "kvr_tree_attention(size)")
+    ws = workspace
+    if ws is None or ws.numel() < nbytes.value:
+        ws = torch.empty(max(nbytes.value, 256), dtype=torch.uint8, device=q.device)
+    elif not ws.is_cuda or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous torch.uint8 CUDA tensor")
+    nbytes.value = ws.numel()
+    rc = call(*args, ws.data_ptr(), nbytes, c.stream(stream, q.device))
+    if rc or check or stream is not None:
+        _finish(c, "kvr_tree_attention", rc, check, status, stream, out, lse, ws)
     return (out, lse) if want_lse else out

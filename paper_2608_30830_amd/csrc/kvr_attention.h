@@ -37,29 +37,27 @@ namespace {
 // other.  Every wave computes the same.
 __device__ Part find_part(const Attention &a, int item)
 {
-    const int lane = threadIdx.x & 63;
-    const int per = part_steps(a);
+    Lane x = lane_sequence(a, 0);
+    const int per = part_steps(a, x);
     int base = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
-        int len = 0, nq = 0, q0 = 0;
-        if (b0 + lane < a.n_seqs) sequence(a, b0 + lane, len, nq, q0);
-        const int steps = steps_of(len, nq), rbs = row_blocks_of(a, nq);
-        const int parts = (steps + per - 1) / per;
-        const int upto = wave_scan(parts * rbs);
+        if (b0) x = lane_sequence(a, b0);
+        const int parts = (x.steps + per - 1) / per;
+        const int upto = wave_incl_scan(parts * x.rbs);
         const uint64_t hit = __ballot(base + upto > item);
         if (hit) {
             const int w = __ffsll((unsigned long long)hit) - 1;
             Part p;
             p.b = b0 + w;
             p.parts = lane_value(parts, w);
-            const int nrb = lane_value(rbs, w);
+            const int nrb = lane_value(x.rbs, w);
             const int at = item - (base + lane_value(upto, w) - p.parts * nrb);
             p.part = at / nrb;
             p.rb = at - p.part * nrb;
-            p.len = lane_value(len, w);
-            p.nq = lane_value(nq, w);
-            p.q0 = lane_value(q0, w);
-            const int s = lane_value(steps, w);
+            p.len = lane_value(x.len, w);
+            p.nq = lane_value(x.nq, w);
+            p.q0 = lane_value(x.q0, w);
+            const int s = lane_value(x.steps, w);
             p.first = (int)((int64_t)s * p.part / p.parts);
             p.last = (int)((int64_t)s * (p.part + 1) / p.parts);
             return p;

@@ -9,13 +9,14 @@ namespace kv {
 namespace {
 
 // Joins the parts of rows.  A row has dim / 4 lanes times Groups groups of parts: each
-// group sums its share of the parts, then the groups are added in order.  With many
-// rows one group does, with few eight keep more loads in flight.
+// group goes through its share of the parts, four at a time, with a running
+// maximum, then the groups are added in order.  With many rows one group does, with
+// few several keep more loads in flight.
 template <int QT, int Groups>
 __global__ __launch_bounds__(256) void combine_kernel(Attention a)
 {
-    __shared__ float so[Groups > 1 ? 1024 : 1];
-    __shared__ float sl[Groups > 1 ? 256 : 1];
+    __shared__ __align__(16) float so[Groups > 1 ? 1024 : 4];
+    __shared__ float sl[Groups > 1 ? 256 : 1], sm[Groups > 1 ? 256 : 1];
     const int dim = a.c.dim, cols = dim / 4;
     const int per_row = cols * Groups;
     const int rows_per_block = 256 / per_row;
@@ -24,14 +25,14 @@ __global__ __launch_bounds__(256) void combine_kernel(Attention a)
     sequence(a, b, len, nq, q0);
     const int rows = nq * a.group;
     if ((int)blockIdx.x * rows_per_block >= rows) return;
-    const int per = part_steps(a);
+    Lane x = lane_sequence(a, 0);
+    const int per = part_steps(a, x);
     const int parts = (steps_of(len, nq) + per - 1) / per;
     if (parts <= 1) return;
     int base = 0;   // items before this sequence's
     for (int b0 = 0; b0 < b; b0 += 64) {
-        int le = 0, nn = 0, qq;
-        if (b0 + lane < b) sequence(a, b0 + lane, le, nn, qq);
-        base += wave_sum((steps_of(le, nn) + per - 1) / per * row_blocks_of(a, nn));
+        if (b0) x = lane_sequence(a, b0);
+        base += wave_total(b0 + lane < b ? (x.steps + per - 1) / per * x.rbs : 0);
     }
     const int local = threadIdx.x / per_row, rest = threadIdx.x - local * per_row;
     const int grp = rest / cols, c = rest - grp * cols;
@@ -39,33 +40,60 @@ __global__ __launch_bounds__(256) void combine_kernel(Attention a)
     const bool live = local < rows_per_block && row < rows;
     const int rb = row / a.block_rows, rr = row - rb * a.block_rows;
     const int nrb = row_blocks_of(a, nq);
-    auto cell = [&](int p) {
-        return ((int64_t)(base + p * nrb + rb) * a.c.n_heads + h) * a.block_rows + rr;
-    };
     f32x4 acc = {0, 0, 0, 0};
     float sum = 0.0f, top = kLowest;
     if (live) {
-        for (int p = 0; p < parts; ++p) top = fmaxf(top, a.part_ml[2 * cell(p)]);
-#pragma unroll 4
-        for (int p = grp; p < parts; p += Groups) {
-            const int64_t at = cell(p);
-            const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * at] - top);
-            sum += f * a.part_ml[2 * at + 1];
-            acc += f * *reinterpret_cast<const f32x4 *>(a.part_o + at * dim + 4 * c);
+        const int64_t first = ((int64_t)(base + rb) * a.c.n_heads + h) * a.block_rows + rr;
+        const int64_t next = (int64_t)nrb * a.c.n_heads * a.block_rows;   // cells from part to part
+        const float *ml = a.part_ml + 2 * first, *o = a.part_o + first * dim + 4 * c;
+        for (int p = grp; p < parts; p += 4 * Groups) {
+            float m[4], l[4];
+            f32x4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t at = min(p + k * Groups, parts - 1) * next;
+                m[k] = ml[2 * at];
+                l[k] = ml[2 * at + 1];
+                v[k] = *reinterpret_cast<const f32x4 *>(o + at * dim);
+            }
+            float t = top;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (p + k * Groups < parts) t = fmaxf(t, m[k]);
+            const float f = __builtin_amdgcn_exp2f(top - t);
+            acc *= f;
+            sum *= f;
+            top = t;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (p + k * Groups < parts) {
+                    const float w = __builtin_amdgcn_exp2f(m[k] - t);
+                    sum += w * l[k];
+                    acc += w * v[k];
+                }
         }
     }
     if constexpr (Groups > 1) {
         if (live) {
             *reinterpret_cast<f32x4 *>(so + 4 * threadIdx.x) = acc;
             sl[threadIdx.x] = sum;
+            sm[threadIdx.x] = top;
         }
         __syncthreads();
         if (!live || grp != 0) return;
+        float t = top;
+#pragma unroll
+        for (int p = 1; p < Groups; ++p) t = fmaxf(t, sm[threadIdx.x + p * cols]);
+        float f = __builtin_amdgcn_exp2f(top - t);
+        acc *= f;
+        sum *= f;
+        top = t;
 #pragma unroll
         for (int p = 1; p < Groups; ++p) {
-            const int t = threadIdx.x + p * cols;
-            acc += *reinterpret_cast<const f32x4 *>(so + 4 * t);
-            sum += sl[t];
+            const int at = threadIdx.x + p * cols;
+            f = __builtin_amdgcn_exp2f(sm[at] - t);
+            acc += f * *reinterpret_cast<const f32x4 *>(so + 4 * at);
+            sum += f * sl[at];
         }
     }
     if (!live) return;
@@ -85,11 +113,12 @@ template <int QT>
 hipError_t launch_combine(const Attention &a, hipStream_t stream)
 {
     const int64_t rows = (int64_t)a.max_q * a.group;
-    const int groups = rows * a.c.n_heads * a.n_seqs >= 4096 || a.c.dim > 128 ? 1 : 8;
-    const int per_block = 256 / (a.c.dim / 4 * groups);
-    const dim3 grid((unsigned)cdiv(rows, std::max(1, per_block)), a.c.n_heads, a.n_seqs);
+    const bool many = rows * a.c.n_heads * a.n_seqs >= 4096;
+    const int groups = many ? 1 : a.c.dim <= 128 ? 8 : 4;   // at most 256 lanes a row
+    const dim3 grid((unsigned)cdiv(rows, 256 / (a.c.dim / 4 * groups)), a.c.n_heads, a.n_seqs);
     if (groups == 1) combine_kernel<QT, 1><<<grid, 256, 0, stream>>>(a);
-    else combine_kernel<QT, 8><<<grid, 256, 0, stream>>>(a);
+    else if (groups == 8) combine_kernel<QT, 8><<<grid, 256, 0, stream>>>(a);
+    else combine_kernel<QT, 4><<<grid, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 

@@ -2,6 +2,7 @@
 // tokens: from the lengths, on the device, the same in every wave.
 #pragma once
 
+#include "kvr_dpp.h"
 #include "kvr_kv_device.h"
 
 namespace kvr {
@@ -22,22 +23,6 @@ struct Part {
     int first, last;  // steps [first, last)
     int len, nq, q0;  // cached tokens, new tokens, first query
 };
-
-__device__ __forceinline__ int wave_sum(int x)
-{
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-    return x;
-}
-__device__ __forceinline__ int wave_scan(int x)   // inclusive
-{
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(x, o);
-        if ((int)(threadIdx.x & 63) >= o) x += y;
-    }
-    return x;
-}
 
 __device__ __forceinline__ int lane_value(int x, int lane)   // uniform
 {
@@ -68,21 +53,33 @@ __device__ __forceinline__ int row_blocks_of(const Attention &a, int nq)
     return (nq * a.group + a.block_rows - 1) / a.block_rows;
 }
 
-// Steps of one part: all sequences' steps (times their row blocks) over the
-// target, at least min_steps.
-__device__ __forceinline__ int part_steps(const Attention &a)
+// 64 sequences, one a lane.
+struct Lane {
+    int len, nq, q0, steps, rbs;
+};
+__device__ __forceinline__ Lane lane_sequence(const Attention &a, int b0)
 {
-    const int lane = threadIdx.x & 63;
-    int64_t total = 0;
-    for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
-        int len = 0, nq = 0, q0;
-        if (b0 + lane < a.n_seqs) sequence(a, b0 + lane, len, nq, q0);
-        // at most 2^26 steps x 2^20 row blocks of 64 sequences: summed in two halves
-        const int64_t w = (int64_t)steps_of(len, nq) * row_blocks_of(a, nq);
-        total += (int64_t)wave_sum((int)(w & 0xffffff)) + ((int64_t)wave_sum((int)(w >> 24)) << 24);
+    Lane x{};
+    const int b = b0 + (threadIdx.x & 63);
+    if (b < a.n_seqs) sequence(a, b, x.len, x.nq, x.q0);
+    x.steps = steps_of(x.len, x.nq);
+    x.rbs = row_blocks_of(a, x.nq);
+    return x;
+}
+
+// Steps of one part: all sequences' steps (times their row blocks) over the
+// target, at least min_steps.  first: the first 64 sequences.
+__device__ __forceinline__ int part_steps(const Attention &a, const Lane &first)
+{
+    int64_t total = wave_total((int64_t)first.steps * first.rbs);
+    for (int b0 = 64; b0 < a.n_seqs; b0 += 64) {
+        const Lane x = lane_sequence(a, b0);
+        total += wave_total((int64_t)x.steps * x.rbs);
     }
-    const int64_t n = (total + a.target - 1) / a.target;
-    return (int)(n > a.min_steps ? n : a.min_steps);
+    // at most 2^12 sequences x 2^26 steps x 2^20 row blocks; the quotient is at most 2^26
+    // and may be one too large: any part size will do
+    const int n = (int)((double)total / (double)a.target) + 1;
+    return n > a.min_steps ? n : a.min_steps;
 }
 
 }  // namespace

@@ -213,12 +213,13 @@ struct Kernel {
     struct State {   // of this wave's rows
         u32x4 q[RT][QS][NB];
         f32x4 o[RT][2 * NB];
-        float m[RT], l[RT];   // reference maximum (log2), this lane's part of the sum
+        float m[RT], l[RT];   // reference maximum (log2), this lane's part of the weights' sum
+        f32x4 w[RT];          // sum of the rounded weights (every element the same)
         int qi[RT];           // query within the sequence
     };
     // LDS: the joining of the waves (maxima, sums, values), or one step of each wave in
     // the order that the matrix instructions read: keys [2][NB][64], values [2 NB][64].
-    static constexpr int JoinWords = 2 * kWaves * BlockRows + BlockRows * LdsRow;
+    static constexpr int JoinWords = 3 * kWaves * BlockRows + BlockRows * LdsRow;
     static constexpr int StepWords = 4 * NB * 64 * 4;
     static constexpr int LdsWords = Shared ? kWaves * StepWords : JoinWords;
 
@@ -464,47 +465,61 @@ struct Kernel {
         }
     }
 
-    // Softmax of one row tile's scores of a step: the weights in the products' type
-    // and the rescaled state.  The reference maximum moves only
-    // when a score exceeds it by more than 8 (a factor of 2^8, which costs the
-    // weights no precision), so most steps need no exchange between lanes.
-    __device__ __forceinline__ void weights(int step, int r, const f32x4 (&sc)[2], State &st,
+    // Before the weights of a step: hidden tokens' scores to -infinity, and the reference
+    // maxima.  Those move only when a score exceeds one by more than 8 (weights of up
+    // to 2^8 lose no precision), so most steps need no exchange between lanes.
+    __device__ __forceinline__ void reference(int step, f32x4 (&sc)[RT][2], State &st) const
+    {
+        if ((step + 1) * kStep > prefix) {
+            // Bits first, then selects: hipcc (ROCm 7.2) loses stores of single elements of
+            // the accumulators under divergent branches.
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                uint32_t seen = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int t = token(step, i);
+                    const bool v = t < len && sees(st.qi[r], t - prefix);
+                    seen |= (v ? 1u : 0u) << i;
+                }
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = seen >> i & 1 ? sc[r][i >> 2][i & 3] : -INFINITY;
+                sc[r][0] = f32x4{x[0], x[1], x[2], x[3]};
+                sc[r][1] = f32x4{x[4], x[5], x[6], x[7]};
+            }
+        }
+        float top[RT];
+        bool moves = false;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const f32x4 x = sc[r][0], y = sc[r][1];
+            top[r] = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+                           fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))) * a.scale2;
+            moves = moves || top[r] > st.m[r] + 8.0f;
+        }
+        if (__ballot(moves)) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const float t = fmaxf(row_max(top[r]), st.m[r]);
+                const float f = __builtin_amdgcn_exp2f(st.m[r] - t);
+                st.l[r] *= f;
+                st.w[r] *= f;
+#pragma unroll
+                for (int e = 0; e < 2 * NB; ++e) st.o[r][e] *= f;
+                st.m[r] = t;
+            }
+        }
+    }
+
+    // The weights of a row tile's scores, in the products' type.
+    __device__ __forceinline__ void weights(int r, const f32x4 (&sc)[2], State &st,
                                             u32x4 (&pv)[QS]) const
     {
         float x[8];
-        uint32_t seen = 0xff;
-        const bool masked = (step + 1) * kStep > prefix;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = sc[i >> 2][i & 3];
-        if (masked) {
-            seen = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int t = token(step, i);
-                const bool v = t < len && sees(st.qi[r], t - prefix);
-                x[i] = v ? x[i] : -INFINITY;
-                seen |= (v ? 1u : 0u) << i;
-            }
-        }
-        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
-                          fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        top = top == -INFINITY ? kLowest : top * a.scale2;
-        if (__ballot(top > st.m[r] + 8.0f)) {
-            top = fmaxf(row_max(top), st.m[r]);
-            const float f = __builtin_amdgcn_exp2f(st.m[r] - top);
-            st.l[r] *= f;
-#pragma unroll
-            for (int e = 0; e < 2 * NB; ++e) st.o[r][e] *= f;
-            st.m[r] = top;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(x[i], a.scale2, -st.m[r]);
-        if (masked) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = seen >> i & 1 ? x[i] : -INFINITY;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __builtin_amdgcn_exp2f(x[i]);
+        for (int i = 0; i < 8; ++i)
+            x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i >> 2][i & 3], a.scale2, -st.m[r]));
         st.l[r] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -517,6 +532,17 @@ struct Kernel {
         }
     }
 
+    // The sum of the weights as they were rounded, by a product with ones: the outputs
+    // are divided by it, so that the rounding of a large weight cancels.
+    __device__ __forceinline__ void count(const u32x4 (&pv)[RT][QS], State &st) const
+    {
+        constexpr uint32_t one = MT == KVR_DT_BF16 ? 0x3f803f80u : 0x3c003c00u;
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int p = 0; p < QS; ++p)
+                st.w[r] = mfma<MT>(u32x4{one, one, one, one}, pv[r][p], st.w[r]);
+    }
     // O^T += V^T P^T of one value tile.
     __device__ __forceinline__ void accumulate(int e, u32x4 x, const u32x4 (&pv)[RT][QS],
                                                State &st) const
@@ -540,9 +566,11 @@ struct Kernel {
                 scores(decltype(I)::value, t, kb, st, sc);
             });
         }
+        reference(step, sc, st);
         u32x4 pv[RT][QS];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) weights(step, r, sc[r], st, pv[r]);
+        for (int r = 0; r < RT; ++r) weights(r, sc[r], st, pv[r]);
+        count(pv, st);
         const bool odd = clean(step, raw.v);
         static_for<0, NB>([&](auto I) {
             u32x4 x[2];
@@ -579,10 +607,10 @@ struct Kernel {
         });
         return odd;
     }
-    __device__ __forceinline__ void compute_shared(int step, const uint32_t *lds, State &st) const
+    __device__ __forceinline__ void scores_shared(const uint32_t *lds, const State &st,
+                                                  f32x4 (&sc)[RT][2]) const
     {
-        const u32x4 *kf = reinterpret_cast<const u32x4 *>(lds) + lane, *vf = kf + 2 * NB * 64;
-        f32x4 sc[RT][2];
+        const u32x4 *kf = reinterpret_cast<const u32x4 *>(lds) + lane;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -590,11 +618,27 @@ struct Kernel {
 #pragma unroll
             for (int i = 0; i < NB; ++i) scores(i, t, kf[(t * NB + i) * 64], st, sc);
         }
+    }
+    // The softmax and values of a step whose scores are sc.  Pipe: the scores of the next
+    // step, in sc afterwards, are formed beside the weights of this one.
+    template <bool Pipe>
+    __device__ __forceinline__ void step_shared(int step, const uint32_t *lds, f32x4 (&sc)[RT][2],
+                                                State &st) const
+    {
+        reference(step, sc, st);
+        f32x4 next[RT][2];
+        if (Pipe) scores_shared(lds + StepWords, st, next);
         u32x4 pv[RT][QS];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) weights(step, r, sc[r], st, pv[r]);
+        for (int r = 0; r < RT; ++r) weights(r, sc[r], st, pv[r]);
+        count(pv, st);
+        const u32x4 *vf = reinterpret_cast<const u32x4 *>(lds) + 2 * NB * 64 + lane;
 #pragma unroll
         for (int e = 0; e < 2 * NB; ++e) accumulate(e, vf[e * 64], pv, st);
+        if (Pipe) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) sc[r][0] = next[r][0], sc[r][1] = next[r][1];
+        }
     }
 
     // Queries of the 16-row tiles from row r0 on; rows past the last repeat it.
@@ -628,6 +672,7 @@ struct Kernel {
             });
             st.m[r] = kLowest;
             st.l[r] = 0.0f;
+            st.w[r] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int e = 0; e < 2 * NB; ++e) st.o[r][e] = f32x4{0, 0, 0, 0};
         }
@@ -636,19 +681,16 @@ struct Kernel {
     // W adjacent elements (2, 4 or 8) of a row of the output, or of a part's.
     template <int W>
     __device__ __forceinline__ void store(const Part &p, int64_t cell, int r0, int row, int d,
-                                          const float *x, float top, float sum) const
+                                          const float *x, float top, float sum, float norm) const
     {
         if (p.parts != 1) {
             float *y = a.part_o + (cell * BlockRows + row) * D + d;
 #pragma unroll
             for (int e = 0; e < W; ++e) y[e] = x[e];
-            if (d == 0) {
-                a.part_ml[(cell * BlockRows + row) * 2] = top;
-                a.part_ml[(cell * BlockRows + row) * 2 + 1] = sum;
-            }
+            if (d == 0) a.part_ml[cell * BlockRows + row] = float4{top, sum, norm, 0.0f};
             return;
         }
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const float inv = norm == 0.0f ? 0.0f : 1.0f / norm;
         const int i0 = (r0 + row) / a.group;
         const int head = h * a.group + (r0 + row - i0 * a.group);
         uint32_t *y = reinterpret_cast<uint32_t *>(
@@ -704,13 +746,15 @@ struct Kernel {
             }
         }
         // join the waves: maxima first, then sums and values in wave order
-        float *sm = lds, *sl = lds + kWaves * BlockRows, *so = lds + 2 * kWaves * BlockRows;
+        float *sm = lds, *sl = sm + kWaves * BlockRows, *sw = sl + kWaves * BlockRows,
+              *so = sw + kWaves * BlockRows;
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             st.l[r] = row_sum(st.l[r]);
             if (g == 0) {
                 sm[wave * BlockRows + 16 * r + n] = st.m[r];
                 sl[wave * BlockRows + 16 * r + n] = st.l[r];
+                sw[wave * BlockRows + 16 * r + n] = st.w[r][0];
             }
         }
         odd = __syncthreads_or(odd);
@@ -747,17 +791,20 @@ struct Kernel {
         for (int i = threadIdx.x; i < BlockRows * (D / 8); i += kThreads) {
             const int row = i / (D / 8), d = 8 * (i - row * (D / 8));
             if (r0 + row >= rows) break;
-            float top = kLowest, sum = 0.0f;
+            float top = kLowest, sum = 0.0f, norm = 0.0f;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm[w * BlockRows + row]);
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w)
-                sum += sl[w * BlockRows + row] * __builtin_amdgcn_exp2f(sm[w * BlockRows + row] - top);
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = __builtin_amdgcn_exp2f(sm[w * BlockRows + row] - top);
+                sum += sl[w * BlockRows + row] * f;
+                norm += sw[w * BlockRows + row] * f;
+            }
             float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = so[row * LdsRow + d + e];
             if (odd) add_odd<8>(p, r0 + row, d, x);
-            store<8>(p, cell, r0, row, d, x, top, sum);
+            store<8>(p, cell, r0, row, d, x, top, sum, norm);
         }
     }
 
@@ -779,8 +826,11 @@ struct Kernel {
             }
             __syncthreads();
             if (active) {
-                const int count = min(kWaves, p.last - s);
-                for (int u = 0; u < count; ++u) compute_shared(s + u, lds + u * StepWords, st);
+                const int last = min(kWaves, p.last - s) - 1;
+                f32x4 sc[RT][2];
+                scores_shared(lds, st, sc);
+                for (int u = 0; u < last; ++u) step_shared<true>(s + u, lds + u * StepWords, sc, st);
+                step_shared<false>(s + last, lds + last * StepWords, sc, st);
             }
             __syncthreads();
         }
@@ -800,7 +850,7 @@ struct Kernel {
                     for (int e = 0; e < W; ++e) x[e] = st.o[r][e0 + e][i];
                     const int d = 16 * e0 + (4 * (int)g + i) * W;
                     if (odd) add_odd<W>(p, r0 + row, d, x);
-                    store<W>(p, cell, r0, row, d, x, st.m[r], sum);
+                    store<W>(p, cell, r0, row, d, x, st.m[r], sum, st.w[r][0]);
                 }
             });
         }

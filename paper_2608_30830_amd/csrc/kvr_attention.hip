@@ -16,7 +16,7 @@ template <int QT, int Groups>
 __global__ __launch_bounds__(256) void combine_kernel(Attention a)
 {
     __shared__ __align__(16) float so[Groups > 1 ? 1024 : 4];
-    __shared__ float sl[Groups > 1 ? 256 : 1], sm[Groups > 1 ? 256 : 1];
+    __shared__ float sl[Groups > 1 ? 256 : 1], sm[Groups > 1 ? 256 : 1], sw[Groups > 1 ? 256 : 1];
     const int dim = a.c.dim, cols = dim / 4;
     const int per_row = cols * Groups;
     const int rows_per_block = 256 / per_row;
@@ -41,34 +41,36 @@ __global__ __launch_bounds__(256) void combine_kernel(Attention a)
     const int rb = row / a.block_rows, rr = row - rb * a.block_rows;
     const int nrb = row_blocks_of(a, nq);
     f32x4 acc = {0, 0, 0, 0};
-    float sum = 0.0f, top = kLowest;
+    float sum = 0.0f, norm = 0.0f, top = kLowest;
     if (live) {
         const int64_t first = ((int64_t)(base + rb) * a.c.n_heads + h) * a.block_rows + rr;
         const int64_t next = (int64_t)nrb * a.c.n_heads * a.block_rows;   // cells from part to part
-        const float *ml = a.part_ml + 2 * first, *o = a.part_o + first * dim + 4 * c;
+        const float4 *ml = a.part_ml + first;
+        const float *o = a.part_o + first * dim + 4 * c;
         for (int p = grp; p < parts; p += 4 * Groups) {
-            float m[4], l[4];
+            float4 m[4];   // maximum, sum of the weights, of the rounded ones
             f32x4 v[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int64_t at = min(p + k * Groups, parts - 1) * next;
-                m[k] = ml[2 * at];
-                l[k] = ml[2 * at + 1];
+                m[k] = ml[at];
                 v[k] = *reinterpret_cast<const f32x4 *>(o + at * dim);
             }
             float t = top;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                if (p + k * Groups < parts) t = fmaxf(t, m[k]);
+                if (p + k * Groups < parts) t = fmaxf(t, m[k].x);
             const float f = __builtin_amdgcn_exp2f(top - t);
             acc *= f;
             sum *= f;
+            norm *= f;
             top = t;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (p + k * Groups < parts) {
-                    const float w = __builtin_amdgcn_exp2f(m[k] - t);
-                    sum += w * l[k];
+                    const float w = __builtin_amdgcn_exp2f(m[k].x - t);
+                    sum += w * m[k].y;
+                    norm += w * m[k].z;
                     acc += w * v[k];
                 }
         }
@@ -78,6 +80,7 @@ __global__ __launch_bounds__(256) void combine_kernel(Attention a)
             *reinterpret_cast<f32x4 *>(so + 4 * threadIdx.x) = acc;
             sl[threadIdx.x] = sum;
             sm[threadIdx.x] = top;
+            sw[threadIdx.x] = norm;
         }
         __syncthreads();
         if (!live || grp != 0) return;
@@ -87,6 +90,7 @@ __global__ __launch_bounds__(256) void combine_kernel(Attention a)
         float f = __builtin_amdgcn_exp2f(top - t);
         acc *= f;
         sum *= f;
+        norm *= f;
         top = t;
 #pragma unroll
         for (int p = 1; p < Groups; ++p) {
@@ -94,10 +98,11 @@ __global__ __launch_bounds__(256) void combine_kernel(Attention a)
             f = __builtin_amdgcn_exp2f(sm[at] - t);
             acc += f * *reinterpret_cast<const f32x4 *>(so + 4 * at);
             sum += f * sl[at];
+            norm += f * sw[at];
         }
     }
     if (!live) return;
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const float inv = norm == 0.0f ? 0.0f : 1.0f / norm;
     const int i0 = row / a.group;
     const int head = h * a.group + (row - i0 * a.group);
     uint32_t *y = reinterpret_cast<uint32_t *>(
@@ -122,7 +127,7 @@ hipError_t launch_combine(const Attention &a, hipStream_t stream)
     return hipGetLastError();
 }
 
-constexpr int kSlots = 1024;   // blocks that the parts are planned for
+constexpr int kSlots = 512;   // resident blocks
 
 }  // namespace
 
@@ -132,8 +137,8 @@ size_t plan_attention(Attention &a)
     a.shared = rows > 32;
     a.row_tiles = rows <= 16 || (rows > 32 && rows <= 64) ? 1 : 2;
     a.block_rows = 16 * a.row_tiles * (a.shared ? kWaves : 1);
-    a.target = std::max(1, kSlots / a.c.n_heads);
-    a.min_steps = 4 * kWaves;
+    a.target = std::max(1, (a.shared && a.row_tiles > 1 ? 2 * kSlots : kSlots) / a.c.n_heads);
+    a.min_steps = kWaves;
     const int64_t longest = cdiv(a.max_kv, kStep);
     // Row blocks of all sequences; ceil(steps / part) parts of each, part = total / target
     // or min_steps.
@@ -142,7 +147,7 @@ size_t plan_attention(Attention &a)
     a.max_items = (int32_t)std::max<int64_t>(
         1, std::min(a.target + blocks, blocks * cdiv(longest, a.min_steps)));
     if (longest <= a.min_steps) return 0;
-    return (size_t)a.max_items * a.c.n_heads * a.block_rows * (a.c.dim + 2) * sizeof(float);
+    return (size_t)a.max_items * a.c.n_heads * a.block_rows * (a.c.dim + 4) * sizeof(float);
 }
 
 hipError_t launch_attention(const Attention &a, hipStream_t stream)

@@ -81,7 +81,8 @@ struct Attention {
     int32_t max_items;           // bound on them
     int32_t min_steps;           // steps that a part has at least
     float *part_o;               // [items][heads][block_rows][dim]
-    float *part_ml;              // [items][heads][block_rows][2]
+    float4 *part_ml;             // [items][heads][block_rows]: maximum, sum of the weights, and
+                                 // of the weights as rounded for the products
     int *status;
 };
 

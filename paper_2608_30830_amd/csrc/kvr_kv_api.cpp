@@ -1,5 +1,6 @@
 // C ABI of the paged KV cache: validation on the host, frequencies of rotary
 // positions, launches.
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -270,12 +271,13 @@ int kvr_tree_attention(const kvr_kv_cache *cache, const kvr_sequences *seqs, con
     a.mask = d_tree_mask;
     a.words = mask_words;
     a.scale2 = (float)(std::fabs((double)scale) * 1.4426950408889634);
+    if (a.scale2 == 0.0f) a.scale2 = FLT_MIN;   // keeps -infinity times it -infinity
     a.negate = scale < 0.0f;
     a.status = d_status;
     if (need) {
-        const size_t cells = need / sizeof(float) / (size_t)(a.c.dim + 2);
+        const size_t cells = need / sizeof(float) / (size_t)(a.c.dim + 4);
         a.part_o = static_cast<float *>(d_ws);
-        a.part_ml = a.part_o + cells * (size_t)a.c.dim;
+        a.part_ml = reinterpret_cast<float4 *>(a.part_o + cells * (size_t)a.c.dim);
     }
     KVR_TRY(kvr::kv::launch_attention(a, static_cast<hipStream_t>(hip_stream)));
     return KVR_OK;

@@ -35,7 +35,7 @@ namespace {
 
 // Where `item` falls: parts of sequences in order, each part's row blocks next to each
 // other.  Every wave computes the same.
-__device__ Part find_part(const Attention &a, int item)
+__device__ __forceinline__ Part find_part(const Attention &a, int item)
 {
     Lane x = lane_sequence(a, 0);
     const int per = part_steps(a, x);
@@ -194,14 +194,14 @@ __device__ __forceinline__ uint32_t perm(uint32_t hi, uint32_t lo, uint32_t sel)
     return __builtin_amdgcn_perm(hi, lo, sel);
 }
 
-template <int FMT, int QT, int NB, int RT, int PF, bool Shared>
+template <int FMT, int QT, int NB, int RT, int PF, bool Shared, int Waves>
 struct Kernel {
     static constexpr int D = NB * 32;
     static constexpr bool Quant = Fmt<FMT>::Quant;
     static constexpr int MT = FMT == KVR_KV_FP16 ? KVR_DT_FP16 : KVR_DT_BF16;   // product type
     // Half-precision queries and weights meet a quantised cache as two bfloat16 parts.
     static constexpr int QS = Quant && QT == KVR_DT_FP16 ? 2 : 1;
-    static constexpr int BlockRows = (Shared ? kWaves : 1) * 16 * RT;
+    static constexpr int BlockRows = (Shared ? Waves : 1) * 16 * RT;
     static constexpr int LdsRow = D + 4;
     using KR = KeyRaw<FMT, NB>;
     using VR = ValRaw<FMT, NB>;
@@ -219,9 +219,9 @@ struct Kernel {
     };
     // LDS: the joining of the waves (maxima, sums, values), or one step of each wave in
     // the order that the matrix instructions read: keys [2][NB][64], values [2 NB][64].
-    static constexpr int JoinWords = 3 * kWaves * BlockRows + BlockRows * LdsRow;
+    static constexpr int JoinWords = 3 * Waves * BlockRows + BlockRows * LdsRow;
     static constexpr int StepWords = 4 * NB * 64 * 4;
-    static constexpr int LdsWords = Shared ? kWaves * StepWords : JoinWords;
+    static constexpr int LdsWords = Shared ? Waves * StepWords : JoinWords;
 
     const Attention &a;
     const uint32_t n, g, lane;
@@ -733,21 +733,21 @@ struct Kernel {
         int s = p.first + wave;
 #pragma unroll
         for (int i = 0; i < PF; ++i)
-            if (s + i * kWaves < p.last) load(s + i * kWaves, raw[i]);
+            if (s + i * Waves < p.last) load(s + i * Waves, raw[i]);
         load_queries(r0, rows, st);
-        for (; s < p.last; s += PF * kWaves) {
+        for (; s < p.last; s += PF * Waves) {
 #pragma unroll
             for (int i = 0; i < PF; ++i) {
-                const int at = s + i * kWaves;
+                const int at = s + i * Waves;
                 if (at < p.last) {
                     odd |= compute(at, raw[i], st);
-                    if (at + PF * kWaves < p.last) load(at + PF * kWaves, raw[i]);
+                    if (at + PF * Waves < p.last) load(at + PF * Waves, raw[i]);
                 }
             }
         }
         // join the waves: maxima first, then sums and values in wave order
-        float *sm = lds, *sl = sm + kWaves * BlockRows, *sw = sl + kWaves * BlockRows,
-              *so = sw + kWaves * BlockRows;
+        float *sm = lds, *sl = sm + Waves * BlockRows, *sw = sl + Waves * BlockRows,
+              *so = sw + Waves * BlockRows;
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             st.l[r] = row_sum(st.l[r]);
@@ -762,12 +762,12 @@ struct Kernel {
         for (int r = 0; r < RT; ++r) {
             float top = kLowest;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm[w * BlockRows + 16 * r + n]);
+            for (int w = 0; w < Waves; ++w) top = fmaxf(top, sm[w * BlockRows + 16 * r + n]);
             const float f = __builtin_amdgcn_exp2f(st.m[r] - top);
 #pragma unroll
             for (int e = 0; e < 2 * NB; ++e) st.o[r][e] *= f;
         }
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < Waves; ++w) {
             if (wave == w) {
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
@@ -788,14 +788,14 @@ struct Kernel {
         }
         // rows out: eight elements a thread
         const int64_t cell = blockIdx.x;
-        for (int i = threadIdx.x; i < BlockRows * (D / 8); i += kThreads) {
+        for (int i = threadIdx.x; i < BlockRows * (D / 8); i += 64 * Waves) {
             const int row = i / (D / 8), d = 8 * (i - row * (D / 8));
             if (r0 + row >= rows) break;
             float top = kLowest, sum = 0.0f, norm = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm[w * BlockRows + row]);
+            for (int w = 0; w < Waves; ++w) top = fmaxf(top, sm[w * BlockRows + row]);
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < Waves; ++w) {
                 const float f = __builtin_amdgcn_exp2f(sm[w * BlockRows + row] - top);
                 sum += sl[w * BlockRows + row] * f;
                 norm += sw[w * BlockRows + row] * f;
@@ -819,14 +819,14 @@ struct Kernel {
         if (p.first + wave < p.last) load(p.first + wave, raw);
         load_queries(r0 + w0, rows, st);
         bool odd = false;
-        for (int s = p.first; s < p.last; s += kWaves) {
+        for (int s = p.first; s < p.last; s += Waves) {
             if (s + wave < p.last) {
                 odd |= put(s + wave, raw, lds + wave * StepWords);
-                if (s + kWaves + wave < p.last) load(s + kWaves + wave, raw);
+                if (s + Waves + wave < p.last) load(s + Waves + wave, raw);
             }
             __syncthreads();
             if (active) {
-                const int last = min(kWaves, p.last - s) - 1;
+                const int last = min(Waves, p.last - s) - 1;
                 f32x4 sc[RT][2];
                 scores_shared(lds, st, sc);
                 for (int u = 0; u < last; ++u) step_shared<true>(s + u, lds + u * StepWords, sc, st);
@@ -865,23 +865,24 @@ constexpr int waves_per_simd()
     return NB * RT > 8 ? 1 : 2;
 }
 
-template <int FMT, int QT, int NB, int RT, int PF, bool Shared>
-__global__ __launch_bounds__(kThreads, (waves_per_simd<NB, RT>())) void attention_kernel(Attention a)
+template <int FMT, int QT, int NB, int RT, int PF, bool Shared, int Waves>
+__global__ __launch_bounds__(64 * Waves, (waves_per_simd<NB, RT>())) void attention_kernel(Attention a)
 {
-    using K = Kernel<FMT, QT, NB, RT, PF, Shared>;
+    using K = Kernel<FMT, QT, NB, RT, PF, Shared, Waves>;
     __shared__ __align__(16) uint32_t lds[K::LdsWords];
     K k(a);
     k.run(lds);
 }
 
-// One launch for a format and query type, the head size and the row tiles chosen here.
-template <int FMT, int QT, int NB, int RT>
+// One launch for a format, query type and head size, by the plan.
+template <int FMT, int QT, int NB, int RT, int Waves>
 hipError_t launch_split(const Attention &a, dim3 grid, hipStream_t stream)
 {
     constexpr int stage = NB * Fmt<FMT>::B8;   // registers of one step's keys and values
-    constexpr int room = (RT == 2 ? (Fmt<FMT>::Quant ? 32 : 64) : Fmt<FMT>::Quant ? 64 : 128) / stage;
+    constexpr int room =
+        (RT == 2 ? (Fmt<FMT>::Quant ? 32 : 64) : Fmt<FMT>::Quant ? 64 : 128) / stage;
     constexpr int PF = room < 1 ? 1 : room > 3 ? 3 : room;
-    attention_kernel<FMT, QT, NB, RT, PF, false><<<grid, kThreads, 0, stream>>>(a);
+    attention_kernel<FMT, QT, NB, RT, PF, false, Waves><<<grid, 64 * Waves, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -890,12 +891,13 @@ hipError_t launch_nb(const Attention &a, dim3 grid, hipStream_t stream)
 {
     if (a.shared) {
         if (a.row_tiles == 1)
-            attention_kernel<FMT, QT, NB, 1, 1, true><<<grid, kThreads, 0, stream>>>(a);
-        else attention_kernel<FMT, QT, NB, 2, 1, true><<<grid, kThreads, 0, stream>>>(a);
+            attention_kernel<FMT, QT, NB, 1, 1, true, 4><<<grid, 256, 0, stream>>>(a);
+        else attention_kernel<FMT, QT, NB, 2, 1, true, 4><<<grid, 256, 0, stream>>>(a);
         return hipGetLastError();
     }
-    if (a.row_tiles == 1) return launch_split<FMT, QT, NB, 1>(a, grid, stream);
-    return launch_split<FMT, QT, NB, 2>(a, grid, stream);
+    if (a.row_tiles == 2) return launch_split<FMT, QT, NB, 2, 4>(a, grid, stream);
+    return a.waves == 8 ? launch_split<FMT, QT, NB, 1, 8>(a, grid, stream)
+                        : launch_split<FMT, QT, NB, 1, 4>(a, grid, stream);
 }
 
 template <int FMT, int QT>

@@ -127,19 +127,27 @@ hipError_t launch_combine(const Attention &a, hipStream_t stream)
     return hipGetLastError();
 }
 
-constexpr int kSlots = 512;   // resident blocks
+constexpr int kSlots = 512;        // resident blocks of four waves
+constexpr int kShortSteps = 16;    // 512 tokens
 
 }  // namespace
 
 size_t plan_attention(Attention &a)
 {
     const int64_t rows = (int64_t)a.max_q * a.group;
+    const int64_t longest = cdiv(a.max_kv, kStep);
     a.shared = rows > 32;
     a.row_tiles = rows <= 16 || (rows > 32 && rows <= 64) ? 1 : 2;
-    a.block_rows = 16 * a.row_tiles * (a.shared ? kWaves : 1);
+    a.waves = 4;
+    a.min_steps = a.waves;
+    // A few short sequences: eight waves a block and no parts, so that one launch does.
+    if (rows <= 16 && longest <= kShortSteps &&
+        (int64_t)a.n_seqs * a.c.n_heads * 2 <= kSlots) {
+        a.waves = 8;
+        a.min_steps = kShortSteps;
+    }
+    a.block_rows = 16 * a.row_tiles * (a.shared ? a.waves : 1);
     a.target = std::max(1, (a.shared && a.row_tiles > 1 ? 2 * kSlots : kSlots) / a.c.n_heads);
-    a.min_steps = kWaves;
-    const int64_t longest = cdiv(a.max_kv, kStep);
     // Row blocks of all sequences; ceil(steps / part) parts of each, part = total / target
     // or min_steps.
     const int64_t blocks = std::min<int64_t>((int64_t)a.n_seqs * cdiv(rows, a.block_rows),

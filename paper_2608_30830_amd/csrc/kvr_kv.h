@@ -76,6 +76,7 @@ struct Attention {
     // launch plan
     int32_t row_tiles;           // 16-row tiles of one wave
     int32_t shared;              // waves share cached tokens and divide rows (else the reverse)
+    int32_t waves;               // of one block
     int32_t block_rows;          // rows of one block
     int32_t target;              // items (a part of a sequence x a block of rows) of one head, about
     int32_t max_items;           // bound on them

@@ -9,8 +9,6 @@ namespace kvr {
 namespace kv {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * 64;
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kLowest = -3.402823466e38f;
 

@@ -268,7 +268,7 @@ def kvr_rotary(x, positions, table, interleaved: bool = False, adjoint: bool = F
     pos = _vector(positions, c.torch.int32, n, "positions")
     t, n_pos, rot = _table(c, table)
     if out is None:
-        out = c.torch.empty((n, h, d), dtype=x.dtype, device=x.device)
+        out = x.new_empty((n, h, d))
         o0, o1 = h * d, d
     else:
         _, (o0, o1, _) = _rows(out, "out", h, d, n)
@@ -327,7 +327,8 @@ def kvr_cache_read(cache: KvCache, slots, dtype=None, out=None, status=None, str
     heads, dim = cache.n_kv_heads, cache.head_dim
     if out is None:
         dtype = c.torch.bfloat16 if dtype is None else dtype
-        k, v = c.torch.empty((2, n, heads, dim), dtype=dtype, device=slots.device)
+        k = slots.new_empty((n, heads, dim), dtype=dtype)
+        v = slots.new_empty((n, heads, dim), dtype=dtype)
         ks = vs = (heads * dim, dim)
     else:
         k, v = out
@@ -375,13 +376,13 @@ def kvr_tree_attention(cache: KvCache, q, cu_q, kv_len, page_table, max_q: int, 
             raise ValueError("tree_mask must be a contiguous [n_queries, words] int64 CUDA tensor")
         mask, words = tree_mask.data_ptr(), tree_mask.shape[1]
     if out is None:
-        out = torch.empty((n, h, d), dtype=q.dtype, device=q.device)
+        out = q.new_empty((n, h, d))
         o0, o1 = h * d, d
     else:
         _, (o0, o1, _) = _rows(out, "out", h, d, n)
         if out.dtype != q.dtype:
             raise ValueError("out must have the type of q")
-    lse = torch.empty((n, h), dtype=torch.float32, device=q.device) if want_lse else None
+    lse = q.new_empty((n, h), dtype=torch.float32) if want_lse else None
     if check or status is not None:
         status = _status(c, check, status, stream)
     s = kvr_sequences(cu, lens, page_table.data_ptr(), stride[0], shape[1], n, seqs, max_q, max_kv)
@@ -395,7 +396,7 @@ def kvr_tree_attention(cache: KvCache, q, cu_q, kv_len, page_table, max_q: int, 
         c.pkg._check(rc, "kvr_tree_attention(size)")
     ws = workspace
     if ws is None or ws.numel() < nbytes.value:
-        ws = torch.empty(max(nbytes.value, 256), dtype=torch.uint8, device=q.device)
+        ws = q.new_empty(max(nbytes.value, 256), dtype=torch.uint8)
     elif not ws.is_cuda or ws.dtype != torch.uint8 or not ws.is_contiguous():
         raise ValueError("workspace must be a contiguous torch.uint8 CUDA tensor")
     nbytes.value = ws.numel()

@@ -238,31 +238,34 @@ struct Kernel {
         vsrow = 4u * (uint32_t)g * (uint32_t)a.c.stoken_stride;
     }
 
-    // The page and the first row in it of the 16 tokens from t on (any tile that
-    // begins at or past the sequence's end is read as its last tile).
-    __device__ __forceinline__ void tile_at(int t, int64_t &page, int &off) const
+    // First tokens of a step's two tiles (any tile that begins at or past the sequence's
+    // end is read as its last tile), and the pages that hold them, as the table has
+    // them: looked up well before the rows are loaded.
+    struct Pages {
+        int id[2];
+    };
+    __device__ __forceinline__ int tile_start(int step, int t) const
     {
-        const int last = (len - 1) & ~15;
-        t = t < last ? t : last;
-        int id = pages[t >> a.c.page_shift];
-        id = __builtin_amdgcn_readfirstlane(id);
-        if (id < 0 || id >= a.c.n_pages) {
-            if (a.status) *a.status = KVR_E_DOMAIN;
-            id = 0;
-        }
-        page = id;
-        off = t & ((1 << a.c.page_shift) - 1);
+        return min(step * kStep + 16 * t, (len - 1) & ~15);
+    }
+    __device__ __forceinline__ Pages look_up(int step) const
+    {
+        return Pages{{pages[tile_start(step, 0) >> a.c.page_shift],
+                      pages[tile_start(step, 1) >> a.c.page_shift]}};
     }
 
-    __device__ __forceinline__ void load(int step, Stage &st) const
+    __device__ __forceinline__ void load(int step, const Pages &where, Stage &st) const
     {
         // Uniform addresses plus one 32-bit lane offset for all keys, one for all values.
         const int64_t ts = a.c.token_stride, sts = a.c.stoken_stride;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            int64_t page;
-            int off;
-            tile_at(step * kStep + 16 * t, page, off);
+            int page = __builtin_amdgcn_readfirstlane(where.id[t]);
+            if (page < 0 || page >= a.c.n_pages) {
+                if (a.status) *a.status = KVR_E_DOMAIN;
+                page = 0;
+            }
+            const int off = tile_start(step, t) & ((1 << a.c.page_shift) - 1);
             const int64_t at = page * a.c.page_stride + h * a.c.head_stride + off * ts;
             const char *kp = a.c.k + at, *vp = a.c.v + at;
             const uint8_t *ksp = nullptr, *vsp = nullptr;
@@ -731,9 +734,15 @@ struct Kernel {
         Stage raw[PF];
         bool odd = false;
         int s = p.first + wave;
+        Pages where[PF];
+#pragma unroll
+        for (int i = 0; i < PF; ++i) where[i] = look_up(s + i * Waves);
 #pragma unroll
         for (int i = 0; i < PF; ++i)
-            if (s + i * Waves < p.last) load(s + i * Waves, raw[i]);
+            if (s + i * Waves < p.last) {
+                load(s + i * Waves, where[i], raw[i]);
+                where[i] = look_up(s + (PF + i) * Waves);
+            }
         load_queries(r0, rows, st);
         for (; s < p.last; s += PF * Waves) {
 #pragma unroll
@@ -741,7 +750,10 @@ struct Kernel {
                 const int at = s + i * Waves;
                 if (at < p.last) {
                     odd |= compute(at, raw[i], st);
-                    if (at + PF * Waves < p.last) load(at + PF * Waves, raw[i]);
+                    if (at + PF * Waves < p.last) {
+                        load(at + PF * Waves, where[i], raw[i]);
+                        where[i] = look_up(at + 2 * PF * Waves);
+                    }
                 }
             }
         }
@@ -816,13 +828,18 @@ struct Kernel {
         const bool active = r0 + w0 < rows;
         State st;
         Stage raw;
-        if (p.first + wave < p.last) load(p.first + wave, raw);
+        Pages where = look_up(p.first + wave);
+        if (p.first + wave < p.last) load(p.first + wave, where, raw);
+        where = look_up(p.first + Waves + wave);
         load_queries(r0 + w0, rows, st);
         bool odd = false;
         for (int s = p.first; s < p.last; s += Waves) {
             if (s + wave < p.last) {
                 odd |= put(s + wave, raw, lds + wave * StepWords);
-                if (s + Waves + wave < p.last) load(s + Waves + wave, raw);
+                if (s + Waves + wave < p.last) {
+                    load(s + Waves + wave, where, raw);
+                    where = look_up(s + 2 * Waves + wave);
+                }
             }
             __syncthreads();
             if (active) {

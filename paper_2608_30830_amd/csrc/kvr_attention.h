@@ -221,7 +221,9 @@ struct Kernel {
     // the order that the matrix instructions read: keys [2][NB][64], values [2 NB][64].
     static constexpr int JoinWords = 3 * Waves * BlockRows + BlockRows * LdsRow;
     static constexpr int StepWords = 4 * NB * 64 * 4;
-    static constexpr int LdsWords = Shared ? Waves * StepWords : JoinWords;
+    static constexpr int Tile = Waves / 2;   // steps that a block brings into LDS at a time
+    static constexpr int Pair = 2;           // steps that are worked on together
+    static constexpr int LdsWords = Shared ? Tile * StepWords : JoinWords;
 
     const Attention &a;
     const uint32_t n, g, lane;
@@ -254,36 +256,42 @@ struct Kernel {
                       pages[tile_start(step, 1) >> a.c.page_shift]}};
     }
 
-    __device__ __forceinline__ void load(int step, const Pages &where, Stage &st) const
+    // Uniform addresses plus one 32-bit lane offset for all keys, one for all values.
+    struct Where {   // a tile in the cache and in its scales
+        int64_t at, sat;
+    };
+    __device__ __forceinline__ Where locate(int step, int t, const Pages &p) const
     {
-        // Uniform addresses plus one 32-bit lane offset for all keys, one for all values.
-        const int64_t ts = a.c.token_stride, sts = a.c.stoken_stride;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            int page = __builtin_amdgcn_readfirstlane(where.id[t]);
-            if (page < 0 || page >= a.c.n_pages) {
-                if (a.status) *a.status = KVR_E_DOMAIN;
-                page = 0;
-            }
-            const int off = tile_start(step, t) & ((1 << a.c.page_shift) - 1);
-            const int64_t at = page * a.c.page_stride + h * a.c.head_stride + off * ts;
-            const char *kp = a.c.k + at, *vp = a.c.v + at;
-            const uint8_t *ksp = nullptr, *vsp = nullptr;
-            if (Quant) {
-                const int64_t sat = page * a.c.spage_stride + h * a.c.shead_stride + off * sts;
-                ksp = a.c.ks + sat;
-                vsp = a.c.vs + sat;
-            }
-            // keys: token n of the tile, chunk g of every slab
+        int page = __builtin_amdgcn_readfirstlane(p.id[t]);
+        if (page < 0 || page >= a.c.n_pages) {
+            if (a.status) *a.status = KVR_E_DOMAIN;
+            page = 0;
+        }
+        const int off = tile_start(step, t) & ((1 << a.c.page_shift) - 1);
+        return Where{page * a.c.page_stride + h * a.c.head_stride + off * a.c.token_stride,
+                     Quant ? page * a.c.spage_stride + h * a.c.shead_stride +
+                                 off * a.c.stoken_stride
+                           : 0};
+    }
+    __device__ __forceinline__ void load_keys(const Where &at, KR &k) const
+    {
+            const char *kp = a.c.k + at.at;
+            const uint8_t *ksp = a.c.ks + at.sat;
+            // token n of the tile, chunk g of every slab
             static_for<0, KR::slabs>([&](auto S) {
                 constexpr int s = decltype(S)::value;
                 constexpr int start = KR::start(s), width = KR::width(s), B8 = Fmt<FMT>::B8;
                 load_words<width * B8>(kp + start * 4 * B8 + (krow + g * (width * B8)),
-                                       &st.k[t].w[start * B8 / 4]);
-                if constexpr (Quant)
-                    st.k[t].s[s] = (ksp + start)[ksrow + (uint32_t)(g * width / 4)];
+                                       &k.w[start * B8 / 4]);
+                if constexpr (Quant) k.s[s] = (ksp + start)[ksrow + (uint32_t)(g * width / 4)];
             });
-            // values: tokens 4 g + j of the tile, chunk n of every slab
+    }
+    __device__ __forceinline__ void load_values(const Where &at, int t, VR &v) const
+    {
+            const int64_t ts = a.c.token_stride, sts = a.c.stoken_stride;
+            const char *vp = a.c.v + at.at;
+            const uint8_t *vsp = a.c.vs + at.sat;
+            // tokens 4 g + j of the tile, chunk n of every slab
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 static_for<0, VR::slabs>([&](auto S) {
@@ -291,12 +299,19 @@ struct Kernel {
                     constexpr int W = VR::width(s), B = Fmt<FMT>::B8 * W / 8;
                     constexpr int e0 = VR::first(s);   // elements / 16 before the slab
                     load_words<B>(vp + j * ts + e0 * 16 * Fmt<FMT>::B8 / 8 + (vrow + n * B),
-                                  &st.v.w[4 * t + j][VR::word(s)]);
+                                  &v.w[4 * t + j][VR::word(s)]);
                     if constexpr (Quant)
-                        st.v.s[4 * t + j][s] =
-                            (vsp + j * sts + e0 / 2)[vsrow + (uint32_t)(n * W / 32)];
+                        v.s[4 * t + j][s] = (vsp + j * sts + e0 / 2)[vsrow + (uint32_t)(n * W / 32)];
                 });
             }
+    }
+    __device__ __forceinline__ void load(int step, const Pages &p, Stage &st) const
+    {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const Where at = locate(step, t, p);
+            load_keys(at, st.k[t]);
+            load_values(at, t, st.v);
         }
     }
 
@@ -468,61 +483,69 @@ struct Kernel {
         }
     }
 
-    // Before the weights of a step: hidden tokens' scores to -infinity, and the reference
-    // maxima.  Those move only when a score exceeds one by more than 8 (weights of up
-    // to 2^8 lose no precision), so most steps need no exchange between lanes.
-    __device__ __forceinline__ void reference(int step, f32x4 (&sc)[RT][2], State &st) const
+    // Before the weights of U steps from `step` on (the part ends before step `last`):
+    // hidden tokens' scores to -infinity, and the reference maxima.  Those move only
+    // when a score exceeds one by more than 8 (weights of up to 2^8 lose no
+    // precision), so most steps need no exchange between lanes.
+    template <int U>
+    __device__ __forceinline__ void reference(int step, int last, f32x4 (&sc)[U][RT][2], State &st) const
     {
-        if ((step + 1) * kStep > prefix) {
+        if ((step + U) * kStep > prefix || step + U > last) {
+            const int end = min(len, last * kStep);
             // Bits first, then selects: hipcc (ROCm 7.2) loses stores of single elements of
             // the accumulators under divergent branches.
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
+            static_for<0, U * RT>([&](auto I) {
+                constexpr int u = decltype(I)::value / RT, r = decltype(I)::value % RT;
                 uint32_t seen = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int t = token(step, i);
-                    const bool v = t < len && sees(st.qi[r], t - prefix);
+                    const int t = token(step + u, i);
+                    const bool v = t < end && sees(st.qi[r], t - prefix);
                     seen |= (v ? 1u : 0u) << i;
                 }
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = seen >> i & 1 ? sc[r][i >> 2][i & 3] : -INFINITY;
-                sc[r][0] = f32x4{x[0], x[1], x[2], x[3]};
-                sc[r][1] = f32x4{x[4], x[5], x[6], x[7]};
-            }
+                const f32x4 x = sc[u][r][0], y = sc[u][r][1];
+                auto pick = [&](int i, float z) { return seen >> i & 1 ? z : -INFINITY; };
+                sc[u][r][0] = f32x4{pick(0, x[0]), pick(1, x[1]), pick(2, x[2]), pick(3, x[3])};
+                sc[u][r][1] = f32x4{pick(4, y[0]), pick(5, y[1]), pick(6, y[2]), pick(7, y[3])};
+            });
         }
         float top[RT];
         bool moves = false;
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const f32x4 x = sc[r][0], y = sc[r][1];
-            top[r] = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
-                           fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3]))) * a.scale2;
+        static_for<0, RT>([&](auto R) {
+            constexpr int r = decltype(R)::value;
+            top[r] = kLowest;
+            static_for<0, U>([&](auto V) {
+                const f32x4 x = sc[decltype(V)::value][r][0], y = sc[decltype(V)::value][r][1];
+                const float z = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+                                      fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+                top[r] = decltype(V)::value ? fmaxf(top[r], z) : z;
+            });
+            top[r] *= a.scale2;
             moves = moves || top[r] > st.m[r] + 8.0f;
-        }
+        });
         if (__ballot(moves)) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
+            static_for<0, RT>([&](auto R) {
+                constexpr int r = decltype(R)::value;
                 const float t = fmaxf(row_max(top[r]), st.m[r]);
                 const float f = __builtin_amdgcn_exp2f(st.m[r] - t);
                 st.l[r] *= f;
                 st.w[r] *= f;
-#pragma unroll
-                for (int e = 0; e < 2 * NB; ++e) st.o[r][e] *= f;
+                static_for<0, 2 * NB>([&](auto E) { st.o[r][decltype(E)::value] *= f; });
                 st.m[r] = t;
-            }
+            });
         }
     }
 
     // The weights of a row tile's scores, in the products' type.
-    __device__ __forceinline__ void weights(int r, const f32x4 (&sc)[2], State &st,
-                                            u32x4 (&pv)[QS]) const
+    template <int R>
+    __device__ __forceinline__ void weights(const f32x4 (&sc)[2], State &st, u32x4 (&pv)[QS]) const
     {
-        float x[8];
+        constexpr int r = R;
+        const f32x4 s0 = sc[0], s1 = sc[1];
+        float x[8] = {s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i >> 2][i & 3], a.scale2, -st.m[r]));
+            x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale2, -st.m[r]));
         st.l[r] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -540,108 +563,113 @@ struct Kernel {
     __device__ __forceinline__ void count(const u32x4 (&pv)[RT][QS], State &st) const
     {
         constexpr uint32_t one = MT == KVR_DT_BF16 ? 0x3f803f80u : 0x3c003c00u;
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int p = 0; p < QS; ++p)
-                st.w[r] = mfma<MT>(u32x4{one, one, one, one}, pv[r][p], st.w[r]);
+        static_for<0, RT * QS>([&](auto I) {
+            constexpr int r = decltype(I)::value / QS, p = decltype(I)::value % QS;
+            st.w[r] = mfma<MT>(u32x4{one, one, one, one}, pv[r][p], st.w[r]);
+        });
     }
     // O^T += V^T P^T of one value tile.
-    __device__ __forceinline__ void accumulate(int e, u32x4 x, const u32x4 (&pv)[RT][QS],
-                                               State &st) const
+    template <int E>
+    __device__ __forceinline__ void accumulate(u32x4 x, const u32x4 (&pv)[RT][QS], State &st) const
     {
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int p = 0; p < QS; ++p) st.o[r][e] = mfma<MT>(x, pv[r][p], st.o[r][e]);
+        static_for<0, RT * QS>([&](auto I) {
+            constexpr int r = decltype(I)::value / QS, p = decltype(I)::value % QS;
+            st.o[r][E] = mfma<MT>(x, pv[r][p], st.o[r][E]);
+        });
     }
 
     // One step from registers; returns whether values were taken out.
     __device__ __forceinline__ bool compute(int step, Stage &raw, State &st) const
     {
-        f32x4 sc[RT][2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) sc[r][t] = f32x4{0, 0, 0, 0};
+        f32x4 sc[1][RT][2];
+        static_for<0, 2>([&](auto T) {
+            constexpr int t = decltype(T)::value;
+            static_for<0, RT>([&](auto R) { sc[0][decltype(R)::value][t] = f32x4{0, 0, 0, 0}; });
             static_for<0, NB>([&](auto I) {
-                const u32x4 kb = key_block<decltype(I)::value>(raw.k[t]);
-                scores(decltype(I)::value, t, kb, st, sc);
+                constexpr int i = decltype(I)::value;
+                scores<i, t>(key_block<i>(raw.k[t]), st, sc[0]);
             });
-        }
-        reference(step, sc, st);
+        });
+        reference<1>(step, step + 1, sc, st);
         u32x4 pv[RT][QS];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) weights(r, sc[r], st, pv[r]);
+        static_for<0, RT>([&](auto R) {
+            weights<decltype(R)::value>(sc[0][decltype(R)::value], st, pv[decltype(R)::value]);
+        });
         count(pv, st);
         const bool odd = clean(step, raw.v);
         static_for<0, NB>([&](auto I) {
             u32x4 x[2];
             val_tiles<decltype(I)::value>(raw.v, x);
-            accumulate(2 * decltype(I)::value, x[0], pv, st);
-            accumulate(2 * decltype(I)::value + 1, x[1], pv, st);
+            accumulate<2 * decltype(I)::value>(x[0], pv, st);
+            accumulate<2 * decltype(I)::value + 1>(x[1], pv, st);
         });
         return odd;
     }
-    __device__ __forceinline__ void scores(int i, int t, u32x4 kb, const State &st,
-                                           f32x4 (&sc)[RT][2]) const
+    template <int I, int T>
+    __device__ __forceinline__ void scores(u32x4 kb, const State &st, f32x4 (&sc)[RT][2]) const
     {
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int p = 0; p < QS; ++p) sc[r][t] = mfma<MT>(kb, st.q[r][p][i], sc[r][t]);
+        static_for<0, RT * QS>([&](auto J) {
+            constexpr int r = decltype(J)::value / QS, p = decltype(J)::value % QS;
+            sc[r][T] = mfma<MT>(kb, st.q[r][p][I], sc[r][T]);
+        });
     }
 
-    // A step into LDS, converted and turned around, and from there.
-    __device__ __forceinline__ bool put(int step, Stage &raw, uint32_t *lds) const
+    // A step's keys or values into LDS, converted and turned around.
+    __device__ __forceinline__ void put_keys(const KR (&k)[2], uint32_t *lds) const
     {
-        u32x4 *kf = reinterpret_cast<u32x4 *>(lds) + lane, *vf = kf + 2 * NB * 64;
-        const bool odd = clean(step, raw.v);
+        u32x4 *kf = reinterpret_cast<u32x4 *>(lds) + lane;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
             static_for<0, NB>([&](auto I) {
-                kf[(t * NB + decltype(I)::value) * 64] = key_block<decltype(I)::value>(raw.k[t]);
+                kf[(t * NB + decltype(I)::value) * 64] = key_block<decltype(I)::value>(k[t]);
             });
+    }
+    __device__ __forceinline__ bool put_values(int step, VR &v, uint32_t *lds) const
+    {
+        u32x4 *vf = reinterpret_cast<u32x4 *>(lds) + 2 * NB * 64 + lane;
+        const bool odd = clean(step, v);
         static_for<0, NB>([&](auto I) {
             u32x4 x[2];
-            val_tiles<decltype(I)::value>(raw.v, x);
+            val_tiles<decltype(I)::value>(v, x);
             vf[(2 * decltype(I)::value) * 64] = x[0];
             vf[(2 * decltype(I)::value + 1) * 64] = x[1];
         });
         return odd;
     }
-    __device__ __forceinline__ void scores_shared(const uint32_t *lds, const State &st,
-                                                  f32x4 (&sc)[RT][2]) const
+    __device__ __forceinline__ void clear_values(uint32_t *lds) const
     {
-        const u32x4 *kf = reinterpret_cast<const u32x4 *>(lds) + lane;
+        u32x4 *vf = reinterpret_cast<u32x4 *>(lds) + 2 * NB * 64 + lane;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) sc[r][t] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < NB; ++i) scores(i, t, kf[(t * NB + i) * 64], st, sc);
-        }
+        for (int e = 0; e < 2 * NB; ++e) vf[e * 64] = u32x4{0, 0, 0, 0};
     }
-    // The softmax and values of a step whose scores are sc.  Pipe: the scores of the next
-    // step, in sc afterwards, are formed beside the weights of this one.
-    template <bool Pipe>
-    __device__ __forceinline__ void step_shared(int step, const uint32_t *lds, f32x4 (&sc)[RT][2],
-                                                State &st) const
+
+    // Two steps from LDS.
+    __device__ __forceinline__ void compute_shared(int step, int last, const uint32_t *lds,
+                                                   State &st) const
     {
-        reference(step, sc, st);
-        f32x4 next[RT][2];
-        if (Pipe) scores_shared(lds + StepWords, st, next);
-        u32x4 pv[RT][QS];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) weights(r, sc[r], st, pv[r]);
-        count(pv, st);
-        const u32x4 *vf = reinterpret_cast<const u32x4 *>(lds) + 2 * NB * 64 + lane;
-#pragma unroll
-        for (int e = 0; e < 2 * NB; ++e) accumulate(e, vf[e * 64], pv, st);
-        if (Pipe) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) sc[r][0] = next[r][0], sc[r][1] = next[r][1];
-        }
+        const u32x4 *f = reinterpret_cast<const u32x4 *>(lds) + lane;
+        f32x4 sc[Pair][RT][2];
+        static_for<0, 2 * Pair>([&](auto I) {
+            constexpr int u = decltype(I)::value / 2, t = decltype(I)::value % 2;
+            static_for<0, RT>([&](auto R) { sc[u][decltype(R)::value][t] = f32x4{0, 0, 0, 0}; });
+            static_for<0, NB>([&](auto I) {
+                constexpr int i = decltype(I)::value;
+                scores<i, t>(f[u * (StepWords / 4) + (t * NB + i) * 64], st, sc[u]);
+            });
+        });
+        reference<Pair>(step, last, sc, st);
+        static_for<0, Pair>([&](auto U) {
+            constexpr int u = decltype(U)::value;
+            u32x4 pv[RT][QS];
+            static_for<0, RT>([&](auto R) {
+                weights<decltype(R)::value>(sc[u][decltype(R)::value], st, pv[decltype(R)::value]);
+            });
+            count(pv, st);
+            static_for<0, 2 * NB>([&](auto E) {
+                constexpr int e = decltype(E)::value;
+                accumulate<e>(f[u * (StepWords / 4) + (2 * NB + e) * 64], pv, st);
+            });
+        });
     }
 
     // Queries of the 16-row tiles from row r0 on; rows past the last repeat it.
@@ -820,44 +848,62 @@ struct Kernel {
         }
     }
 
-    // Many rows: the waves divide the block's rows; each brings one step of a group of
-    // four into LDS, and all of them work on all four.
+    // The loop of a wave that brings the keys (or the values) of step `mine` of every
+    // tile into LDS.  Two copies of it, so that the keys and the values in flight take
+    // the same registers.
+    template <bool Keys>
+    __device__ __forceinline__ bool walk(const Part &p, int mine, bool active, uint32_t *lds,
+                                         State &st) const
+    {
+        std::conditional_t<Keys, Stage, VR> raw;   // of Stage only the keys
+        bool odd = false;
+        Pages where = look_up(p.first + mine);
+        auto fetch = [&](int s) {
+            if (s + mine >= p.last) return;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const Where at = locate(s + mine, t, where);
+                if constexpr (Keys) load_keys(at, raw.k[t]);
+                else load_values(at, t, raw);
+            }
+            where = look_up(s + Tile + mine);
+        };
+        fetch(p.first);
+        for (int s = p.first; s < p.last; s += Tile) {
+            uint32_t *to = lds + mine * StepWords;
+            if (s + mine < p.last) {
+                if constexpr (Keys) put_keys(raw.k, to);
+                else odd = put_values(s + mine, raw, to) || odd;
+            } else if (!Keys) {
+                clear_values(to);   // beyond the part: weights of zero meet zeros
+            }
+            fetch(s + Tile);
+            __syncthreads();
+            if (active)
+                for (int u = 0; u < Tile && s + u < p.last; u += Pair)
+                    compute_shared(s + u, p.last, lds + u * StepWords, st);
+            __syncthreads();
+        }
+        return odd;
+    }
+
+    // Many rows: the waves divide the block's rows and all work on every step; half of
+    // them bring keys into LDS and half values.
     __device__ __forceinline__ void run_shared(const Part &p, int wave, int r0, int rows, uint32_t *lds)
     {
         const int w0 = 16 * RT * wave;
         const bool active = r0 + w0 < rows;
         State st;
-        Stage raw;
-        Pages where = look_up(p.first + wave);
-        if (p.first + wave < p.last) load(p.first + wave, where, raw);
-        where = look_up(p.first + Waves + wave);
         load_queries(r0 + w0, rows, st);
-        bool odd = false;
-        for (int s = p.first; s < p.last; s += Waves) {
-            if (s + wave < p.last) {
-                odd |= put(s + wave, raw, lds + wave * StepWords);
-                if (s + Waves + wave < p.last) {
-                    load(s + Waves + wave, where, raw);
-                    where = look_up(s + 2 * Waves + wave);
-                }
-            }
-            __syncthreads();
-            if (active) {
-                const int last = min(Waves, p.last - s) - 1;
-                f32x4 sc[RT][2];
-                scores_shared(lds, st, sc);
-                for (int u = 0; u < last; ++u) step_shared<true>(s + u, lds + u * StepWords, sc, st);
-                step_shared<false>(s + last, lds + last * StepWords, sc, st);
-            }
-            __syncthreads();
-        }
+        bool odd = wave < Tile ? walk<true>(p, wave, active, lds, st)
+                               : walk<false>(p, wave - Tile, active, lds, st);
         odd = __syncthreads_or(odd);
         const int64_t cell = blockIdx.x;
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
+        static_for<0, RT>([&](auto R) {
+            constexpr int r = decltype(R)::value;
             const int row = w0 + 16 * r + (int)n;
             const float sum = row_sum(st.l[r]);
-            if (r0 + row >= rows) continue;
+            if (r0 + row >= rows) return;
             static_for<0, VR::slabs>([&](auto S) {
                 constexpr int e0 = VR::first(decltype(S)::value), W = VR::width(decltype(S)::value);
 #pragma unroll
@@ -870,20 +916,12 @@ struct Kernel {
                     store<W>(p, cell, r0, row, d, x, st.m[r], sum, st.w[r][0]);
                 }
             });
-        }
+        });
     }
 };
 
-// Waves per SIMD that the registers are bounded for: two, or one where a wave's
-// accumulators, queries and rows in flight need more than 256.
-template <int NB, int RT>
-constexpr int waves_per_simd()
-{
-    return NB * RT > 8 ? 1 : 2;
-}
-
 template <int FMT, int QT, int NB, int RT, int PF, bool Shared, int Waves>
-__global__ __launch_bounds__(64 * Waves, (waves_per_simd<NB, RT>())) void attention_kernel(Attention a)
+__global__ __launch_bounds__(64 * Waves, 2) void attention_kernel(Attention a)
 {
     using K = Kernel<FMT, QT, NB, RT, PF, Shared, Waves>;
     __shared__ __align__(16) uint32_t lds[K::LdsWords];
@@ -895,10 +933,11 @@ __global__ __launch_bounds__(64 * Waves, (waves_per_simd<NB, RT>())) void attent
 template <int FMT, int QT, int NB, int RT, int Waves>
 hipError_t launch_split(const Attention &a, dim3 grid, hipStream_t stream)
 {
+    // steps in flight: what the registers left by queries and accumulators hold
     constexpr int stage = NB * Fmt<FMT>::B8;   // registers of one step's keys and values
-    constexpr int room =
-        (RT == 2 ? (Fmt<FMT>::Quant ? 32 : 64) : Fmt<FMT>::Quant ? 64 : 128) / stage;
-    constexpr int PF = room < 1 ? 1 : room > 3 ? 3 : room;
+    constexpr bool quant = Fmt<FMT>::Quant, two = quant && QT == KVR_DT_FP16;
+    constexpr int room = (RT == 2 ? (quant ? 32 : 64) : quant ? 64 : 128) / stage;
+    constexpr int PF = room < 1 || NB * (two ? 2 : 1) > 8 || NB == 8 ? 1 : room > 3 ? 3 : room;
     attention_kernel<FMT, QT, NB, RT, PF, false, Waves><<<grid, 64 * Waves, 0, stream>>>(a);
     return hipGetLastError();
 }
@@ -906,13 +945,17 @@ hipError_t launch_split(const Attention &a, dim3 grid, hipStream_t stream)
 template <int FMT, int QT, int NB>
 hipError_t launch_nb(const Attention &a, dim3 grid, hipStream_t stream)
 {
+    if constexpr (NB <= 4) {   // heads beyond 128 take one row tile a wave
+        if (a.row_tiles == 2 && a.shared) {
+            attention_kernel<FMT, QT, NB, 2, 1, true, 4><<<grid, 256, 0, stream>>>(a);
+            return hipGetLastError();
+        }
+        if (a.row_tiles == 2) return launch_split<FMT, QT, NB, 2, 4>(a, grid, stream);
+    }
     if (a.shared) {
-        if (a.row_tiles == 1)
-            attention_kernel<FMT, QT, NB, 1, 1, true, 4><<<grid, 256, 0, stream>>>(a);
-        else attention_kernel<FMT, QT, NB, 2, 1, true, 4><<<grid, 256, 0, stream>>>(a);
+        attention_kernel<FMT, QT, NB, 1, 1, true, 4><<<grid, 256, 0, stream>>>(a);
         return hipGetLastError();
     }
-    if (a.row_tiles == 2) return launch_split<FMT, QT, NB, 2, 4>(a, grid, stream);
     return a.waves == 8 ? launch_split<FMT, QT, NB, 1, 8>(a, grid, stream)
                         : launch_split<FMT, QT, NB, 1, 4>(a, grid, stream);
 }

@@ -136,8 +136,12 @@ size_t plan_attention(Attention &a)
 {
     const int64_t rows = (int64_t)a.max_q * a.group;
     const int64_t longest = cdiv(a.max_kv, kStep);
-    a.shared = rows > 32;
-    a.row_tiles = rows <= 16 || (rows > 32 && rows <= 64) ? 1 : 2;
+    // Up to 16 rows: every wave has them all, and a share of the cached tokens.  Up to 32 the
+    // same with two row tiles, where registers allow (heads up to 128).  Beyond, waves
+    // share the tokens through LDS.
+    const bool narrow = a.c.dim <= 128;
+    a.shared = rows > (narrow ? 32 : 16);
+    a.row_tiles = rows <= 16 || !narrow || (rows > 32 && rows <= 64) ? 1 : 2;
     a.waves = 4;
     a.min_steps = a.waves;
     // A few short sequences: eight waves a block and no parts, so that one launch does.
@@ -147,7 +151,7 @@ size_t plan_attention(Attention &a)
         a.min_steps = kShortSteps;
     }
     a.block_rows = 16 * a.row_tiles * (a.shared ? a.waves : 1);
-    a.target = std::max(1, (a.shared && a.row_tiles > 1 ? 2 * kSlots : kSlots) / a.c.n_heads);
+    a.target = std::max(1, (a.shared ? a.row_tiles > 1 ? 2 * kSlots : kSlots * 3 / 2 : kSlots) / a.c.n_heads);
     // Row blocks of all sequences; ceil(steps / part) parts of each, part = total / target
     // or min_steps.
     const int64_t blocks = std::min<int64_t>((int64_t)a.n_seqs * cdiv(rows, a.block_rows),

@@ -389,7 +389,8 @@ int kvr_cost_grid_noalloc(const double *d_wait_s, const int32_t *d_ctx_tokens, i
  *
  * Conventions of these entry points, beside the shared ones above: strides of
  * activations count elements, those of a cache bytes; the elements of a row are
- * adjacent; counts may be zero (nothing is launched).  Device-detected errors
+ * adjacent, and the stride of a dimension of one element does not matter; counts may
+ * be zero (nothing is launched).  Device-detected errors
  * (a position outside the table, a slot or page outside the pool, lengths that
  * do not fit the call) are reported through d_status, device int32[1] or NULL:
  * the kernels store KVR_E_DOMAIN there and never clear it, and nothing outside
@@ -459,7 +460,7 @@ enum { KVR_ROTARY_INTERLEAVED = 1,   /* pairs (2i, 2i + 1); else (i, i + rot_dim
  *                  the elements from rot_dim on are copied.
  *   Rows that are 16-byte aligned, head_dim a multiple of 8 and rot_dim of 16 (8
  *   interleaved) go eight elements at a time, others one pair at a time.
- *   Sizes: n_tokens * n_heads <= 2^31 - 1, n_heads <= 65,536, head_dim <= 65,536.
+ *   Sizes: n_tokens * n_heads <= 2^31 - 1, n_heads <= 65,536, head_dim <= 4,096.
  */
 int kvr_rotary(const void *d_x, void *d_out, int32_t dtype, int64_t n_tokens, int32_t n_heads,
                int32_t head_dim, int64_t x_token_stride, int64_t x_head_stride,
@@ -537,7 +538,8 @@ typedef struct {
  *   d_ws, ws_bytes  workspace (two-phase sizing as above; contents need not be
  *                  set).  It may be 0 bytes: then d_ws is not used, any non-NULL
  *                  256-byte aligned pointer will do.
- *   Sizes: n_q_heads a multiple of n_kv_heads, max_q * n_q_heads <= 2^24.
+ *   Sizes: n_q_heads a multiple of n_kv_heads, max_q * n_q_heads <= 2^24, max_kv <=
+ *   2^30.  The workspace is sized from the host fields of seqs and the cache.
  */
 int kvr_tree_attention(const kvr_kv_cache *cache, const kvr_sequences *seqs, const void *d_q,
                        int32_t dtype, int32_t n_q_heads, int64_t q_token_stride,

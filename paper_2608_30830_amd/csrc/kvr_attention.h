@@ -16,10 +16,19 @@
 // become bfloat16 by the format conversions, which apply the block's power of
 // two on the way and are exact.
 //
-// Each wave takes every n-th step of 32 tokens and keeps the loads of the next
-// steps in flight; a block joins its waves through LDS.  The sequences are cut
-// along the cached tokens into about as many equal parts as fill the GPU (from
-// the lengths, on the device); combine_kernel joins the parts.
+// With up to 32 rows every wave has all of them and takes every n-th step of 32
+// tokens, with the loads of the next steps in flight and their pages looked up a
+// round earlier; a block joins its waves through LDS.  Memory bounds this: 64
+// sequences of 8,192 tokens, 8 heads of 128, one new token each: 187 us in 8
+// bits (5.9 TB/s of cache), 374 us in 16 (5.7), 120 us in 4 (4.8, where the
+// conversions begin to count).  With more rows the waves divide them and share
+// the tokens through LDS, converted and turned around once: 16 sequences of
+// 16,384 tokens and 512 rows, 16 bits: 0.75 ms, 725 TFLOP/s, bound by the vector
+// instructions of the softmax, the matrix instructions and the LDS reads, which
+// overlap only in part.
+//
+// The sequences are cut along the cached tokens into about as many equal parts as
+// fill the GPU (from the lengths, on the device); combine_kernel joins the parts.
 //
 // Each source that includes this header builds the kernel for one cache format
 // and query type.
@@ -273,37 +282,37 @@ struct Kernel {
                                  off * a.c.stoken_stride
                            : 0};
     }
+    // Token n of the tile, chunk g of every slab.
     __device__ __forceinline__ void load_keys(const Where &at, KR &k) const
     {
-            const char *kp = a.c.k + at.at;
-            const uint8_t *ksp = a.c.ks + at.sat;
-            // token n of the tile, chunk g of every slab
-            static_for<0, KR::slabs>([&](auto S) {
-                constexpr int s = decltype(S)::value;
-                constexpr int start = KR::start(s), width = KR::width(s), B8 = Fmt<FMT>::B8;
-                load_words<width * B8>(kp + start * 4 * B8 + (krow + g * (width * B8)),
-                                       &k.w[start * B8 / 4]);
-                if constexpr (Quant) k.s[s] = (ksp + start)[ksrow + (uint32_t)(g * width / 4)];
-            });
+        const char *kp = a.c.k + at.at;
+        const uint8_t *ksp = a.c.ks + at.sat;
+        static_for<0, KR::slabs>([&](auto S) {
+            constexpr int s = decltype(S)::value;
+            constexpr int start = KR::start(s), width = KR::width(s), B8 = Fmt<FMT>::B8;
+            load_words<width * B8>(kp + start * 4 * B8 + (krow + g * (width * B8)),
+                                   &k.w[start * B8 / 4]);
+            if constexpr (Quant) k.s[s] = (ksp + start)[ksrow + (uint32_t)(g * width / 4)];
+        });
     }
+    // Tokens 4 g + j of the tile, chunk n of every slab.
     __device__ __forceinline__ void load_values(const Where &at, int t, VR &v) const
     {
-            const int64_t ts = a.c.token_stride, sts = a.c.stoken_stride;
-            const char *vp = a.c.v + at.at;
-            const uint8_t *vsp = a.c.vs + at.sat;
-            // tokens 4 g + j of the tile, chunk n of every slab
+        const int64_t ts = a.c.token_stride, sts = a.c.stoken_stride;
+        const char *vp = a.c.v + at.at;
+        const uint8_t *vsp = a.c.vs + at.sat;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                static_for<0, VR::slabs>([&](auto S) {
-                    constexpr int s = decltype(S)::value;
-                    constexpr int W = VR::width(s), B = Fmt<FMT>::B8 * W / 8;
-                    constexpr int e0 = VR::first(s);   // elements / 16 before the slab
-                    load_words<B>(vp + j * ts + e0 * 16 * Fmt<FMT>::B8 / 8 + (vrow + n * B),
-                                  &v.w[4 * t + j][VR::word(s)]);
-                    if constexpr (Quant)
-                        v.s[4 * t + j][s] = (vsp + j * sts + e0 / 2)[vsrow + (uint32_t)(n * W / 32)];
-                });
-            }
+        for (int j = 0; j < 4; ++j) {
+            static_for<0, VR::slabs>([&](auto S) {
+                constexpr int s = decltype(S)::value;
+                constexpr int W = VR::width(s), B = Fmt<FMT>::B8 * W / 8;
+                constexpr int e0 = VR::first(s);   // elements / 16 before the slab
+                load_words<B>(vp + j * ts + e0 * 16 * Fmt<FMT>::B8 / 8 + (vrow + n * B),
+                              &v.w[4 * t + j][VR::word(s)]);
+                if constexpr (Quant)
+                    v.s[4 * t + j][s] = (vsp + j * sts + e0 / 2)[vsrow + (uint32_t)(n * W / 32)];
+            });
+        }
     }
     __device__ __forceinline__ void load(int step, const Pages &p, Stage &st) const
     {

@@ -127,7 +127,12 @@ hipError_t launch_combine(const Attention &a, hipStream_t stream)
     return hipGetLastError();
 }
 
-constexpr int kSlots = 512;        // resident blocks of four waves
+// Blocks that the parts are planned for, of all heads: what is resident at once (two
+// blocks on each of 256 CUs, three where 64 rows share tokens), so that equal parts
+// end together; twice that where each block has 128 rows, because there the rows of
+// ragged sequences fill blocks unevenly (tree of up to 64 tokens over 2,048 to 32,768:
+// 501 us planned for 512, 417 for 1,024, 423 for 2,048 and more joining).
+constexpr int kSlots = 512;
 constexpr int kShortSteps = 16;    // 512 tokens
 
 }  // namespace
@@ -138,24 +143,28 @@ size_t plan_attention(Attention &a)
     const int64_t longest = cdiv(a.max_kv, kStep);
     // Up to 16 rows: every wave has them all, and a share of the cached tokens.  Up to 32 the
     // same with two row tiles, where registers allow (heads up to 128).  Beyond, waves
-    // share the tokens through LDS.
+    // share the tokens through LDS (56 rows over 131,071 tokens in 4 bits: 66 us against
+    // 74 with two row tiles a wave).
     const bool narrow = a.c.dim <= 128;
     a.shared = rows > (narrow ? 32 : 16);
     a.row_tiles = rows <= 16 || !narrow || (rows > 32 && rows <= 64) ? 1 : 2;
     a.waves = 4;
     a.min_steps = a.waves;
-    // A few short sequences: eight waves a block and no parts, so that one launch does.
-    if (rows <= 16 && longest <= kShortSteps &&
-        (int64_t)a.n_seqs * a.c.n_heads * 2 <= kSlots) {
+    int slots = kSlots;
+    if (a.shared) slots = a.row_tiles > 1 ? 2 * kSlots : kSlots * 3 / 2;
+    // A few short sequences: eight waves a block and no parts, so that one launch does (one
+    // sequence of 500 tokens: 12.7 us a call against 14.8 in parts; of 1,000: 16.5, 14.7).
+    if (rows <= 16 && longest <= kShortSteps && (int64_t)a.n_seqs * a.c.n_heads * 2 <= kSlots) {
         a.waves = 8;
         a.min_steps = kShortSteps;
     }
     a.block_rows = 16 * a.row_tiles * (a.shared ? a.waves : 1);
-    a.target = std::max(1, (a.shared ? a.row_tiles > 1 ? 2 * kSlots : kSlots * 3 / 2 : kSlots) / a.c.n_heads);
+    a.target = std::max(1, slots / a.c.n_heads);
     // Row blocks of all sequences; ceil(steps / part) parts of each, part = total / target
     // or min_steps.
     const int64_t blocks = std::min<int64_t>((int64_t)a.n_seqs * cdiv(rows, a.block_rows),
                                              a.n_queries * a.group / a.block_rows + a.n_seqs);
+    // (at most 2^30 launched blocks: 2^12 sequences x 2^24 query heads and tokens / 64 rows)
     a.max_items = (int32_t)std::max<int64_t>(
         1, std::min(a.target + blocks, blocks * cdiv(longest, a.min_steps)));
     if (longest <= a.min_steps) return 0;

@@ -34,24 +34,27 @@ int check_cache(const kvr_kv_cache *c, Cache &out)
     const int32_t hd = c->head_dim;
     if (hd != 64 && hd != 96 && hd != 128 && hd != 192 && hd != 256) return KVR_E_LAYOUT;
     if (!aligned16(c->k_data) || !aligned16(c->v_data)) return KVR_E_LAYOUT;
-    const int64_t st[3] = {c->page_stride, c->head_stride, c->token_stride};
+    // strides of a single page or head do not matter
+    const int64_t page = c->n_pages > 1 ? c->page_stride : 0;
+    const int64_t head = c->n_kv_heads > 1 ? c->head_stride : 0;
+    const int64_t spage = c->n_pages > 1 ? c->scale_page_stride : 0;
+    const int64_t shead = c->n_kv_heads > 1 ? c->scale_head_stride : 0;
+    const int64_t st[3] = {page, head, c->token_stride};
     for (int64_t s : st)
         if (s < 0 || s % 16 != 0) return KVR_E_LAYOUT;
     if (c->token_stride > (1 << 26)) return KVR_E_LAYOUT;
-    if (quant) {
-        if (c->scale_page_stride < 0 || c->scale_head_stride < 0 || c->scale_token_stride < 0 ||
-            c->scale_token_stride > (1 << 26))
-            return KVR_E_LAYOUT;
-    }
+    if (quant && (spage < 0 || shead < 0 || c->scale_token_stride < 0 ||
+                  c->scale_token_stride > (1 << 26)))
+        return KVR_E_LAYOUT;
     out.k = static_cast<char *>(c->k_data);
     out.v = static_cast<char *>(c->v_data);
     out.ks = static_cast<uint8_t *>(c->k_scale);
     out.vs = static_cast<uint8_t *>(c->v_scale);
-    out.page_stride = c->page_stride;
-    out.head_stride = c->head_stride;
+    out.page_stride = page;
+    out.head_stride = head;
     out.token_stride = c->token_stride;
-    out.spage_stride = c->scale_page_stride;
-    out.shead_stride = c->scale_head_stride;
+    out.spage_stride = spage;
+    out.shead_stride = shead;
     out.stoken_stride = c->scale_token_stride;
     out.n_pages = c->n_pages;
     out.page_shift = __builtin_ctz((unsigned)ps);
@@ -61,9 +64,12 @@ int check_cache(const kvr_kv_cache *c, Cache &out)
     return KVR_OK;
 }
 
-Rows rows(const void *p, int64_t token, int64_t head, int32_t dtype)
+// The strides of a single token or head do not matter.
+Rows rows(const void *p, int64_t tokens, int64_t token_stride, int64_t heads, int64_t head_stride,
+          int32_t dtype)
 {
-    return Rows{static_cast<char *>(const_cast<void *>(p)), token, head, dtype};
+    return Rows{static_cast<char *>(const_cast<void *>(p)), tokens > 1 ? token_stride : 0,
+                heads > 1 ? head_stride : 0, dtype};
 }
 
 bool rows_aligned(const Rows &r)
@@ -155,7 +161,7 @@ int kvr_rotary(const void *d_x, void *d_out, int32_t dtype, int64_t n_tokens, in
                const float *d_table, int64_t n_pos, int32_t rot_dim, int32_t flags,
                int32_t *d_status, void *hip_stream)
 {
-    if (n_tokens < 0 || n_heads < 1 || n_heads > 65536 || head_dim < 2 || head_dim > 65536 ||
+    if (n_tokens < 0 || n_heads < 1 || n_heads > 65536 || head_dim < 2 || head_dim > 4096 ||
         n_tokens > kMaxRows / n_heads)
         return KVR_E_SIZE;
     if (!dtype_ok(dtype)) return KVR_E_LAYOUT;
@@ -164,9 +170,9 @@ int kvr_rotary(const void *d_x, void *d_out, int32_t dtype, int64_t n_tokens, in
     if (!d_x || !d_out || !d_table) return KVR_E_NULL;
     int rc = check_rotary(d_pos, d_table, n_pos, rot_dim, head_dim, flags, r);
     if (rc != KVR_OK) return rc;
-    const Rows x = rows(d_x, x_token_stride, x_head_stride, dtype);
-    const Rows out = rows(d_out, out_token_stride, out_head_stride, dtype);
-    if (x_token_stride < 0 || x_head_stride < 0 || out_token_stride < 0 || out_head_stride < 0)
+    const Rows x = rows(d_x, n_tokens, x_token_stride, n_heads, x_head_stride, dtype);
+    const Rows out = rows(d_out, n_tokens, out_token_stride, n_heads, out_head_stride, dtype);
+    if (x.token_stride < 0 || x.head_stride < 0 || out.token_stride < 0 || out.head_stride < 0)
         return KVR_E_LAYOUT;
     const uintptr_t odd = (uintptr_t)(dtype_bytes(dtype) - 1);
     if ((reinterpret_cast<uintptr_t>(d_x) | reinterpret_cast<uintptr_t>(d_out)) & odd)
@@ -194,8 +200,8 @@ int kvr_cache_write(const kvr_kv_cache *cache, const void *d_k, const void *d_v,
         rc = check_rotary(d_pos, d_table, n_pos, rot_dim, c.dim, flags, r);
         if (rc != KVR_OK) return rc;
     }
-    const Rows k = rows(d_k, k_token_stride, k_head_stride, dtype);
-    const Rows v = rows(d_v, v_token_stride, v_head_stride, dtype);
+    const Rows k = rows(d_k, n_tokens, k_token_stride, c.n_heads, k_head_stride, dtype);
+    const Rows v = rows(d_v, n_tokens, v_token_stride, c.n_heads, v_head_stride, dtype);
     if (!rows_aligned(k) || !rows_aligned(v)) return KVR_E_LAYOUT;
     KVR_TRY(kvr::kv::launch_cache_write(c, k, v, n_tokens, d_slots, r, d_status,
                                         static_cast<hipStream_t>(hip_stream)));
@@ -214,8 +220,8 @@ int kvr_cache_read(const kvr_kv_cache *cache, const int64_t *d_slots, int64_t n_
     if (!dtype_ok(dtype)) return KVR_E_LAYOUT;
     if (n_tokens == 0) return KVR_OK;
     if (!d_k || !d_v || !d_slots) return KVR_E_NULL;
-    const Rows k = rows(d_k, k_token_stride, k_head_stride, dtype);
-    const Rows v = rows(d_v, v_token_stride, v_head_stride, dtype);
+    const Rows k = rows(d_k, n_tokens, k_token_stride, c.n_heads, k_head_stride, dtype);
+    const Rows v = rows(d_v, n_tokens, v_token_stride, c.n_heads, v_head_stride, dtype);
     if (!rows_aligned(k) || !rows_aligned(v)) return KVR_E_LAYOUT;
     KVR_TRY(kvr::kv::launch_cache_read(c, k, v, n_tokens, d_slots, d_status,
                                        static_cast<hipStream_t>(hip_stream)));
@@ -239,7 +245,7 @@ int kvr_tree_attention(const kvr_kv_cache *cache, const kvr_sequences *seqs, con
         return KVR_E_LAYOUT;
     if (n_q_heads < a.c.n_heads || n_q_heads % a.c.n_heads != 0) return KVR_E_SIZE;
     if (seqs->n_seqs < 0 || seqs->n_seqs > kvr::kv::kMaxSeqs || seqs->max_q < 1 ||
-        seqs->max_kv < 1 || seqs->max_kv > INT32_MAX - 64 || seqs->n_queries < 0 ||
+        seqs->max_kv < 1 || seqs->max_kv > (1 << 30) || seqs->n_queries < 0 ||
         seqs->n_queries > INT32_MAX || seqs->max_pages < 0 || seqs->pages_stride < 0 ||
         (int64_t)seqs->max_q * n_q_heads > (1 << 24))
         return KVR_E_SIZE;
@@ -259,8 +265,8 @@ int kvr_tree_attention(const kvr_kv_cache *cache, const kvr_sequences *seqs, con
     if ((reinterpret_cast<uintptr_t>(d_ws) & 255) != 0 || *ws_bytes < need) return KVR_E_WORKSPACE;
     if (seqs->n_seqs == 0 || seqs->n_queries == 0) return KVR_OK;
     if (!d_q || !d_out || !seqs->d_cu_q || !seqs->d_kv_len || !seqs->d_pages) return KVR_E_NULL;
-    a.q = rows(d_q, q_token_stride, q_head_stride, dtype);
-    a.out = rows(d_out, out_token_stride, out_head_stride, dtype);
+    a.q = rows(d_q, a.n_queries, q_token_stride, n_q_heads, q_head_stride, dtype);
+    a.out = rows(d_out, a.n_queries, out_token_stride, n_q_heads, out_head_stride, dtype);
     if (!rows_aligned(a.q) || !rows_aligned(a.out)) return KVR_E_LAYOUT;
     a.lse = d_lse;
     a.cu_q = seqs->d_cu_q;

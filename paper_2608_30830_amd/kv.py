@@ -154,6 +154,12 @@ def _finish(x, name, rc, check, status, stream, *tensors):
         x.pkg._check(int(status.item()), f"{name}(device)")
 
 
+def _alike(a, b):
+    """Same shape and, where they matter, the same strides."""
+    return a.shape == b.shape and all(n <= 1 or x == y for n, x, y in
+                                      zip(a.shape, a.stride(), b.stride()))
+
+
 class KvCache:
     """The tensors of a paged cache, kept alive with the C view of them.
 
@@ -165,7 +171,7 @@ class KvCache:
 
     def __init__(self, k, v, k_scale=None, v_scale=None):
         import torch
-        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype or v.stride() != k.stride():
+        if k.dim() != 4 or v.dtype != k.dtype or not _alike(k, v):
             raise ValueError("k and v must be [n_pages, n_kv_heads, page_size, row] alike")
         if not k.is_cuda or not v.is_cuda or k.stride(3) != 1:
             raise ValueError("k and v must be CUDA tensors with adjacent rows")
@@ -177,8 +183,8 @@ class KvCache:
                 raise ValueError("a quantised cache needs k_scale and v_scale")
             s = k_scale
             if s.dim() != 4 or s.shape[:3] != k.shape[:3] or s.dtype != torch.uint8 or \
-                    not s.is_cuda or not v_scale.is_cuda or v_scale.shape != s.shape or \
-                    v_scale.dtype != s.dtype or v_scale.stride() != s.stride() or \
+                    not s.is_cuda or not v_scale.is_cuda or v_scale.dtype != s.dtype or \
+                    not _alike(s, v_scale) or \
                     (s.shape[3] > 1 and s.stride(3) != 1):
                 raise ValueError("k_scale and v_scale must be [n_pages, n_kv_heads, page_size, "
                                  "head_dim / 32] uint8 CUDA tensors alike")

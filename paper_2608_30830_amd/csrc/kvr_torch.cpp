@@ -1,0 +1,342 @@
+// The KV cache's entry points on torch tensors: checks of types, shapes and strides,
+// outputs and workspaces from torch's allocator, torch's current stream, then the C ABI.
+// A call costs about what its launches cost: from Python, one launch takes 2.5 us,
+// reading the tensors and filling in the C arguments another 4 us through ctypes and
+// below 1 us here.
+#include <Python.h>
+
+#include <ATen/ATen.h>
+#include <ATen/core/LegacyTypeDispatch.h>
+#include <c10/hip/HIPStream.h>
+#include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <string>
+
+#include "kvr.h"
+
+namespace {
+
+// A bad argument: a ValueError (or TypeError) with this text.
+struct Refused {
+    PyObject *type;
+    std::string text;
+};
+[[noreturn]] void refuse(const std::string &text) { throw Refused{PyExc_ValueError, text}; }
+
+const at::Tensor &tensor(PyObject *o, const char *name)
+{
+    if (!THPVariable_Check(o)) throw Refused{PyExc_TypeError, std::string(name) + " must be a tensor"};
+    return THPVariable_Unpack(o);
+}
+bool given(PyObject *o) { return o != Py_None; }
+
+int64_t integer(PyObject *o, const char *name)
+{
+    const long long x = PyLong_AsLongLong(o);
+    if (x == -1 && PyErr_Occurred()) {
+        PyErr_Clear();
+        throw Refused{PyExc_TypeError, std::string(name) + " must be an integer"};
+    }
+    return x;
+}
+int32_t integer32(PyObject *o, const char *name)
+{
+    const int64_t x = integer(o, name);
+    if (x < INT32_MIN || x > INT32_MAX) refuse(std::string(name) + " is beyond 32 bits");
+    return (int32_t)x;
+}
+
+int32_t dtype_of(const at::Tensor &t, const char *name)
+{
+    switch (t.scalar_type()) {
+    case at::kBFloat16: return KVR_DT_BF16;
+    case at::kHalf: return KVR_DT_FP16;
+    case at::kFloat: return KVR_DT_FP32;
+    default:
+        refuse(std::string(name) + " must be bfloat16, float16 or float32, not " +
+               std::string(c10::toString(t.scalar_type())));
+    }
+}
+
+// A [tokens, heads, dim] tensor with adjacent rows; sizes below 0 are free.
+const at::Tensor &rows(PyObject *o, const char *name, int64_t tokens, int64_t heads, int64_t dim)
+{
+    const at::Tensor &t = tensor(o, name);
+    if (!t.is_cuda() || t.dim() != 3 || (t.stride(2) != 1 && t.size(2) != 1))
+        refuse(std::string(name) + " must be a [tokens, heads, dim] CUDA tensor with adjacent rows");
+    const int64_t want[3] = {tokens, heads, dim};
+    for (int i = 0; i < 3; ++i)
+        if (want[i] >= 0 && t.size(i) != want[i]) {
+            auto one = [](int64_t n) { return n < 0 ? std::string("any") : std::to_string(n); };
+            refuse(std::string(name) + " must have shape (" + one(tokens) + ", " + one(heads) + ", " +
+                   one(dim) + "), not (" + std::to_string(t.size(0)) + ", " +
+                   std::to_string(t.size(1)) + ", " + std::to_string(t.size(2)) + ")");
+        }
+    return t;
+}
+
+// Address of a contiguous [count] tensor.
+template <class T>
+T *vector(PyObject *o, const char *name, at::ScalarType type, int64_t count)
+{
+    const at::Tensor &t = tensor(o, name);
+    if (!t.is_cuda() || t.scalar_type() != type || t.dim() != 1 || t.size(0) != count ||
+        !t.is_contiguous())
+        refuse(std::string(name) + " must be a contiguous [" + std::to_string(count) + "] " +
+               c10::toString(type) + " CUDA tensor");
+    return static_cast<T *>(t.data_ptr());
+}
+int32_t *status_of(PyObject *o)
+{
+    return given(o) ? vector<int32_t>(o, "status", at::kInt, 1) : nullptr;
+}
+
+struct Table {
+    const float *t = nullptr;
+    int64_t n_pos = 0;
+    int32_t rot = 0;
+};
+Table table_of(PyObject *o)
+{
+    const at::Tensor &t = tensor(o, "table");
+    if (!t.is_cuda() || t.scalar_type() != at::kFloat || t.dim() != 3 || t.size(1) != 2 ||
+        !t.is_contiguous() || t.size(2) > (1 << 20))
+        refuse("table must be a contiguous [n_pos, 2, rot_dim / 2] float32 CUDA tensor");
+    return Table{static_cast<const float *>(t.data_ptr()), t.size(0), (int32_t)(2 * t.size(2))};
+}
+
+const kvr_kv_cache *cache_of(PyObject *o)
+{
+    const void *p = PyLong_AsVoidPtr(o);
+    if (!p) {
+        PyErr_Clear();
+        throw Refused{PyExc_TypeError, "cache must be a KvCache"};
+    }
+    return static_cast<const kvr_kv_cache *>(p);
+}
+
+// The caller's stream (its handle), or torch's current one on the tensor's device.
+void *stream_of(PyObject *o, const at::Tensor &t)
+{
+    if (given(o)) return PyLong_AsVoidPtr(o);
+    return c10::hip::getCurrentHIPStream(t.device().index()).stream();
+}
+
+// A Python tuple of a status code and tensors (undefined ones: None).
+template <class... Ts>
+PyObject *answer(int rc, const Ts &...ts)
+{
+    PyObject *r = PyTuple_New(1 + sizeof...(ts));
+    if (!r) return nullptr;
+    PyTuple_SET_ITEM(r, 0, PyLong_FromLong(rc));
+    int i = 1;
+    auto put = [&](const at::Tensor &t) {
+        PyObject *o = Py_None;
+        if (t.defined()) o = THPVariable_Wrap(t);
+        else Py_INCREF(o);
+        PyTuple_SET_ITEM(r, i++, o);
+    };
+    (put(ts), ...);
+    return r;
+}
+
+// No C++ exception leaves an entry point.
+template <class F>
+PyObject *entry(Py_ssize_t got, Py_ssize_t want, F f)
+{
+    if (got != want) {
+        PyErr_Format(PyExc_TypeError, "%zd arguments expected, not %zd", want, got);
+        return nullptr;
+    }
+    HANDLE_TH_ERRORS
+    try {
+        const at::AutoDispatchBelowADInplaceOrView plain;   // nothing here records gradients
+        return f();
+    } catch (const Refused &e) {
+        PyErr_SetString(e.type, e.text.c_str());
+        return nullptr;
+    }
+    END_HANDLE_TH_ERRORS
+}
+
+at::Tensor out_like(PyObject *o, const at::Tensor &x, const char *message)
+{
+    if (!given(o)) return at::empty(x.sizes(), x.options().memory_format(at::MemoryFormat::Contiguous));
+    at::Tensor out = rows(o, "out", x.size(0), x.size(1), x.size(2));
+    if (out.scalar_type() != x.scalar_type()) refuse(message);
+    return out;
+}
+
+int32_t fits32(int64_t n, const char *name)
+{
+    if (n > INT32_MAX) refuse(std::string(name) + " is beyond 32 bits");
+    return (int32_t)n;
+}
+
+// (x, positions, table, flags, out, status, stream) -> (code, out)
+PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 7, [&] {
+        const at::Tensor &x = rows(a[0], "x", -1, -1, -1);
+        const int32_t dt = dtype_of(x, "x");
+        const int64_t tokens = x.size(0);
+        const int32_t *pos = vector<int32_t>(a[1], "positions", at::kInt, tokens);
+        const Table t = table_of(a[2]);
+        const at::Tensor out = out_like(a[4], x, "out must have the type of x");
+        const int rc = kvr_rotary(x.data_ptr(), out.data_ptr(), dt, tokens,
+                                  fits32(x.size(1), "heads"), fits32(x.size(2), "head_dim"),
+                                  x.stride(0), x.stride(1), out.stride(0), out.stride(1), pos, t.t,
+                                  t.n_pos, t.rot, integer32(a[3], "flags"), status_of(a[5]),
+                                  stream_of(a[6], x));
+        return answer(rc, out);
+    });
+}
+
+// (cache, k, v, slots, positions, table, flags, status, stream) -> (code,)
+PyObject *cache_write(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 9, [&] {
+        const kvr_kv_cache *c = cache_of(a[0]);
+        const at::Tensor &slots = tensor(a[3], "slots");
+        const int64_t tokens = slots.dim() ? slots.size(0) : 0;
+        const at::Tensor &k = rows(a[1], "k", tokens, c->n_kv_heads, c->head_dim);
+        const at::Tensor &v = rows(a[2], "v", tokens, c->n_kv_heads, c->head_dim);
+        const int32_t dt = dtype_of(k, "k");
+        if (v.scalar_type() != k.scalar_type()) refuse("k and v must have one type");
+        const int64_t *at = vector<int64_t>(a[3], "slots", at::kLong, tokens);
+        const int32_t *pos = nullptr;
+        Table t;
+        if (given(a[5])) {
+            t = table_of(a[5]);
+            if (!given(a[4])) refuse("a table needs positions");
+            pos = vector<int32_t>(a[4], "positions", at::kInt, tokens);
+        } else if (given(a[4])) {
+            refuse("positions need a table");
+        }
+        return answer(kvr_cache_write(c, k.data_ptr(), v.data_ptr(), dt, tokens, k.stride(0),
+                                      k.stride(1), v.stride(0), v.stride(1), at, pos, t.t, t.n_pos,
+                                      t.rot, integer32(a[6], "flags"), status_of(a[7]),
+                                      stream_of(a[8], slots)));
+    });
+}
+
+// (cache, slots, KVR_DT_* or None, out k, out v, status, stream) -> (code, k, v)
+PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 7, [&] {
+        const kvr_kv_cache *c = cache_of(a[0]);
+        const at::Tensor &slots = tensor(a[1], "slots");
+        const int64_t tokens = slots.dim() ? slots.size(0) : 0;
+        const int64_t *at = vector<int64_t>(a[1], "slots", at::kLong, tokens);
+        const int64_t heads = c->n_kv_heads, dim = c->head_dim;
+        at::Tensor k, v;
+        int32_t dt;
+        if (!given(a[3])) {
+            dt = given(a[2]) ? integer32(a[2], "dtype") : KVR_DT_BF16;
+            const at::ScalarType type = dt == KVR_DT_BF16   ? at::kBFloat16
+                                        : dt == KVR_DT_FP16 ? at::kHalf
+                                                            : at::kFloat;
+            const auto options = slots.options().dtype(type);
+            k = at::empty({tokens, heads, dim}, options);
+            v = at::empty({tokens, heads, dim}, options);
+        } else {
+            k = rows(a[3], "out k", tokens, heads, dim);
+            v = rows(a[4], "out v", tokens, heads, dim);
+            dt = dtype_of(k, "out");
+            if (v.scalar_type() != k.scalar_type() || (given(a[2]) && integer32(a[2], "dtype") != dt))
+                refuse("out must be two tensors of the type that is asked for");
+        }
+        const int rc = kvr_cache_read(c, at, tokens, k.data_ptr(), v.data_ptr(), dt, k.stride(0),
+                                      k.stride(1), v.stride(0), v.stride(1), status_of(a[5]),
+                                      stream_of(a[6], slots));
+        return answer(rc, k, v);
+    });
+}
+
+// (cache, q, cu_q, kv_len, page_table, max_q, max_kv, tree_mask, scale, want_lse, out,
+// workspace, status, stream) -> (code, out, lse, workspace)
+PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 14, [&] {
+        const kvr_kv_cache *c = cache_of(a[0]);
+        const at::Tensor &q = rows(a[1], "q", -1, -1, c->head_dim);
+        const int32_t dt = dtype_of(q, "q");
+        const at::Tensor &len = tensor(a[3], "kv_len");
+        const int64_t seqs = len.dim() ? len.size(0) : 0;
+        kvr_sequences s{};
+        s.d_kv_len = vector<int32_t>(a[3], "kv_len", at::kInt, seqs);
+        s.d_cu_q = vector<int32_t>(a[2], "cu_q", at::kInt, seqs + 1);
+        const at::Tensor &pages = tensor(a[4], "page_table");
+        if (!pages.is_cuda() || pages.scalar_type() != at::kInt || pages.dim() != 2 ||
+            pages.size(0) != seqs || (pages.size(1) > 1 && pages.stride(1) != 1))
+            refuse("page_table must be a [n_seqs, pages] int32 CUDA tensor");
+        s.d_pages = static_cast<const int32_t *>(pages.data_ptr());
+        s.pages_stride = pages.stride(0);
+        s.max_pages = pages.size(1);
+        s.n_queries = q.size(0);
+        s.n_seqs = fits32(seqs, "n_seqs");
+        s.max_q = integer32(a[5], "max_q");
+        s.max_kv = integer32(a[6], "max_kv");
+        const uint64_t *mask = nullptr;
+        int32_t words = 0;
+        if (given(a[7])) {
+            const at::Tensor &m = tensor(a[7], "tree_mask");
+            if (!m.is_cuda() || m.scalar_type() != at::kLong || m.dim() != 2 ||
+                m.size(0) != s.n_queries || !m.is_contiguous())
+                refuse("tree_mask must be a contiguous [n_queries, words] int64 CUDA tensor");
+            mask = static_cast<const uint64_t *>(m.data_ptr());
+            words = fits32(m.size(1), "tree_mask");
+        }
+        double scale = 1.0 / std::sqrt((double)c->head_dim);
+        if (given(a[8])) {
+            scale = PyFloat_AsDouble(a[8]);
+            if (scale == -1.0 && PyErr_Occurred()) {
+                PyErr_Clear();
+                throw Refused{PyExc_TypeError, "scale must be a number"};
+            }
+        }
+        const at::Tensor out = out_like(a[10], q, "out must have the type of q");
+        at::Tensor lse, ws;
+        if (PyObject_IsTrue(a[9]))
+            lse = at::empty({q.size(0), q.size(1)}, q.options().dtype(at::kFloat));
+        const int32_t heads = fits32(q.size(1), "q");
+        size_t bytes = 0;
+        auto call = [&](void *space) {
+            return kvr_tree_attention(c, &s, q.data_ptr(), dt, heads, q.stride(0), q.stride(1), mask,
+                                      words, (float)scale, out.data_ptr(), out.stride(0),
+                                      out.stride(1),
+                                      lse.defined() ? static_cast<float *>(lse.data_ptr()) : nullptr,
+                                      status_of(a[12]), space, &bytes, stream_of(a[13], q));
+        };
+        int rc = call(nullptr);   // the workspace's size
+        if (rc != KVR_OK) return answer(rc, out, lse, ws);
+        if (given(a[11])) {
+            ws = tensor(a[11], "workspace");
+            if (!ws.is_cuda() || ws.scalar_type() != at::kByte || !ws.is_contiguous())
+                refuse("workspace must be a contiguous torch.uint8 CUDA tensor");
+        }
+        if (bytes == 0) {   // nothing is cut: an address that is never used
+            alignas(256) static char none[256];
+            return answer(call(none), out, lse, at::Tensor());
+        }
+        if (!ws.defined() || (size_t)ws.numel() < bytes)
+            ws = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte));
+        bytes = (size_t)ws.numel();
+        rc = call(ws.data_ptr());
+        return answer(rc, out, lse, ws);
+    });
+}
+
+#define KVR_FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
+PyMethodDef kMethods[] = {KVR_FAST(rotary), KVR_FAST(cache_write), KVR_FAST(cache_read),
+                          KVR_FAST(tree_attention), {nullptr, nullptr, 0, nullptr}};
+PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "kvr_torch", nullptr, -1, kMethods,
+                       nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+extern "C" PyObject *PyInit_kvr_torch() { return PyModule_Create(&kModule); }

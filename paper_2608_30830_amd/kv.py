@@ -1,4 +1,5 @@
-"""Binding of the paged KV cache's entry points of libkvr: argument marshalling only.
+"""Binding of the paged KV cache's entry points of libkvr: argument marshalling only,
+the most of it in the built module ``kvr_torch``, which takes tensors.
 
 A :class:`KvCache` names the tensors of a cache; ``kvr_cache_write``,
 ``kvr_cache_read`` and ``kvr_tree_attention`` work on it, ``kvr_rotary`` on
@@ -10,8 +11,12 @@ With ``check`` (the default) a call waits and raises on a device-detected error;
 from __future__ import annotations
 
 import ctypes
-import math
+import importlib.machinery
+import importlib.util
+import os
 from typing import Optional
+
+BINDING_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_build", "kvr_torch.so")
 
 KVR_DT_BF16 = 0
 KVR_DT_FP16 = 1
@@ -75,25 +80,32 @@ def declare(lib) -> None:
         getattr(lib, name).restype = ctypes.c_int
 
 
+def load_binding():
+    """The built module that takes torch tensors to these entry points (raises if it
+    has not been built)."""
+    import torch  # noqa: F401  (its libraries, before the module that needs them)
+    import paper_2608_30830_amd as pkg
+    pkg.load_library()
+    if not os.path.exists(BINDING_PATH):
+        raise RuntimeError(f"the binding is not built ({BINDING_PATH}); run __graft_entry__.build()")
+    loader = importlib.machinery.ExtensionFileLoader("kvr_torch", BINDING_PATH)
+    spec = importlib.util.spec_from_loader("kvr_torch", loader)
+    module = importlib.util.module_from_spec(spec)
+    loader.exec_module(module)
+    return module
+
+
 class _Context:
-    """torch, the package and the loaded library, looked up once."""
+    """torch, the package, the loaded library and its binding, looked up once."""
 
     def __init__(self):
         import torch
         import paper_2608_30830_amd as pkg
         pkg._torch()   # raises without a GPU
         self.torch, self.pkg, self.lib = torch, pkg, pkg.load_library()
+        self.fast = load_binding()
         self.codes = {torch.bfloat16: KVR_DT_BF16, torch.float16: KVR_DT_FP16,
                       torch.float32: KVR_DT_FP32}
-        # the current stream's handle without making a Stream object (2.7 us less a call)
-        self.raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-
-    def stream(self, stream, device):
-        if stream is not None:
-            return stream.cuda_stream
-        if self.raw is not None:
-            return self.raw(device.index)
-        return self.torch.cuda.current_stream(device).cuda_stream
 
 
 _CTX: Optional[_Context] = None
@@ -106,37 +118,9 @@ def _context() -> _Context:
     return _CTX
 
 
-def _dtype(x, t, name):
-    """The KVR_DT_* of a tensor."""
-    code = x.codes.get(t.dtype)
-    if code is None:
-        raise ValueError(f"{name} must be bfloat16, float16 or float32, not {t.dtype}")
-    return code
-
-
-def _rows(t, name, heads=None, dim=None, tokens=None):
-    """Shape and strides of a [tokens, heads, dim] device tensor with adjacent rows."""
-    shape, stride = t.shape, t.stride()
-    if not t.is_cuda or len(shape) != 3 or (stride[2] != 1 and shape[2] != 1):
-        raise ValueError(f"{name} must be a [tokens, heads, dim] CUDA tensor with adjacent rows")
-    if (tokens is not None and shape[0] != tokens) or (heads is not None and shape[1] != heads) or (
-            dim is not None and shape[2] != dim):
-        raise ValueError(f"{name} must have shape {(tokens, heads, dim)}, not {tuple(shape)}")
-    return shape, stride
-
-
-def _vector(t, dtype, count, name):
-    """Address of a contiguous [count] device tensor."""
-    if not t.is_cuda or t.dtype != dtype or t.shape != (count,) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous [{count}] {dtype} CUDA tensor")
-    return t.data_ptr()
-
-
 def _status(x, check, status, stream):
     """The status tensor of a call: the caller's, or with check a new one."""
-    if status is not None:
-        _vector(status, x.torch.int32, 1, "status")
-    elif check:
+    if status is None and check:
         status = x.torch.zeros(1, dtype=x.torch.int32, device="cuda")
         if stream is not None:   # zeroed on the current stream
             stream.wait_stream(x.torch.cuda.current_stream())
@@ -207,7 +191,7 @@ class KvCache:
         c.n_pages, c.page_size, c.n_kv_heads, c.head_dim = pages, page, heads, dim
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = pages, heads, page, dim
         self.format = c.format
-        self.ref = ctypes.byref(c)
+        self.address = ctypes.addressof(c)
 
     @classmethod
     def allocate(cls, fmt: int, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int):
@@ -247,44 +231,28 @@ def kvr_rotary_table(rot_dim: int, n_pos: int, theta: float = 10000.0,
     table = x.torch.empty((n_pos, 2, rot_dim // 2), dtype=x.torch.float32, device="cuda")
     rope = kvr_rope(theta, factor, low, high, trained_len, magnitude, kind)
     rc = x.lib.kvr_rotary_table(ctypes.byref(rope), rot_dim, n_pos, table.data_ptr(),
-                                x.stream(stream, table.device))
+                                x.pkg._stream_ptr(stream))
     _finish(x, "kvr_rotary_table", rc, False, None, stream, table)
     return table
-
-
-def _table(x, table):
-    """Address, positions and rotated elements of a rotary table."""
-    shape = table.shape
-    if not table.is_cuda or table.dtype != x.torch.float32 or len(shape) != 3 or shape[1] != 2 or \
-            not table.is_contiguous():
-        raise ValueError("table must be a contiguous [n_pos, 2, rot_dim / 2] float32 CUDA tensor")
-    return table.data_ptr(), shape[0], 2 * shape[2]
 
 
 def _flags(interleaved, adjoint):
     return (KVR_ROTARY_INTERLEAVED if interleaved else 0) | (KVR_ROTARY_ADJOINT if adjoint else 0)
 
 
+def _handle(stream):
+    """A stream's handle; None: torch's current stream."""
+    return None if stream is None else stream.cuda_stream
+
+
 def kvr_rotary(x, positions, table, interleaved: bool = False, adjoint: bool = False, out=None,
                status=None, stream=None, check: bool = True):
     """x [tokens, heads, dim] turned by its positions; ``out`` may be ``x``."""
     c = _context()
-    (n, h, d), xs = _rows(x, "x")
-    dt = _dtype(c, x, "x")
-    pos = _vector(positions, c.torch.int32, n, "positions")
-    t, n_pos, rot = _table(c, table)
-    if out is None:
-        out = x.new_empty((n, h, d))
-        o0, o1 = h * d, d
-    else:
-        _, (o0, o1, _) = _rows(out, "out", h, d, n)
-        if out.dtype != x.dtype:
-            raise ValueError("out must have the type of x")
-    if check or status is not None:
+    if check:
         status = _status(c, check, status, stream)
-    rc = c.lib.kvr_rotary(x.data_ptr(), out.data_ptr(), dt, n, h, d, xs[0], xs[1], o0, o1, pos, t,
-                          n_pos, rot, _flags(interleaved, adjoint),
-                          None if status is None else status.data_ptr(), c.stream(stream, x.device))
+    rc, out = c.fast.rotary(x, positions, table, _flags(interleaved, adjoint), out, status,
+                            _handle(stream))
     if rc or check or stream is not None:
         _finish(c, "kvr_rotary", rc, check, status, stream, out)
     return out
@@ -297,28 +265,10 @@ def kvr_cache_write(cache: KvCache, k, v, slots, positions=None, table=None,
     page_size + row; below 0: not written); with ``table`` the keys are rotated by
     ``positions`` on the way."""
     c = _context()
-    n = slots.shape[0]
-    _, ks = _rows(k, "k", cache.n_kv_heads, cache.head_dim, n)
-    _, vs = _rows(v, "v", cache.n_kv_heads, cache.head_dim, n)
-    dt = _dtype(c, k, "k")
-    if v.dtype != k.dtype:
-        raise ValueError("k and v must have one type")
-    at = _vector(slots, c.torch.int64, n, "slots")
-    pos = t = None
-    n_pos = rot = 0
-    if table is not None:
-        t, n_pos, rot = _table(c, table)
-        if positions is None:
-            raise ValueError("a table needs positions")
-        pos = _vector(positions, c.torch.int32, n, "positions")
-    elif positions is not None:
-        raise ValueError("positions need a table")
-    if check or status is not None:
+    if check:
         status = _status(c, check, status, stream)
-    rc = c.lib.kvr_cache_write(cache.ref, k.data_ptr(), v.data_ptr(), dt, n, ks[0], ks[1], vs[0],
-                               vs[1], at, pos, t, n_pos, rot, _flags(interleaved, adjoint),
-                               None if status is None else status.data_ptr(),
-                               c.stream(stream, slots.device))
+    rc, = c.fast.cache_write(cache.address, k, v, slots, positions, table,
+                             _flags(interleaved, adjoint), status, _handle(stream))
     if rc or check or stream is not None:
         _finish(c, "kvr_cache_write", rc, check, status, stream)
 
@@ -328,26 +278,14 @@ def kvr_cache_read(cache: KvCache, slots, dtype=None, out=None, status=None, str
     """(k, v) of ``slots`` [tokens] int64, each [tokens, n_kv_heads, head_dim] in
     ``dtype`` (bfloat16 by default); below 0: zeros.  ``out``: a pair to write to."""
     c = _context()
-    n = slots.shape[0]
-    at = _vector(slots, c.torch.int64, n, "slots")
-    heads, dim = cache.n_kv_heads, cache.head_dim
-    if out is None:
-        dtype = c.torch.bfloat16 if dtype is None else dtype
-        k = slots.new_empty((n, heads, dim), dtype=dtype)
-        v = slots.new_empty((n, heads, dim), dtype=dtype)
-        ks = vs = (heads * dim, dim)
-    else:
-        k, v = out
-        _, ks = _rows(k, "out k", heads, dim, n)
-        _, vs = _rows(v, "out v", heads, dim, n)
-        if v.dtype != k.dtype or (dtype is not None and k.dtype != dtype):
-            raise ValueError("out must be two tensors of the type that is asked for")
-    dt = _dtype(c, k, "out")
-    if check or status is not None:
+    if check:
         status = _status(c, check, status, stream)
-    rc = c.lib.kvr_cache_read(cache.ref, at, n, k.data_ptr(), v.data_ptr(), dt, ks[0], ks[1], vs[0],
-                              vs[1], None if status is None else status.data_ptr(),
-                              c.stream(stream, slots.device))
+    if dtype is not None:
+        if dtype not in c.codes:
+            raise ValueError(f"out must be bfloat16, float16 or float32, not {dtype}")
+        dtype = c.codes[dtype]
+    k, v = (None, None) if out is None else out
+    rc, k, v = c.fast.cache_read(cache.address, slots, dtype, k, v, status, _handle(stream))
     if rc or check or stream is not None:
         _finish(c, "kvr_cache_read", rc, check, status, stream, k, v)
     return k, v
@@ -365,48 +303,11 @@ def kvr_tree_attention(cache: KvCache, q, cu_q, kv_len, page_table, max_q: int, 
     ``scale`` defaults to head_dim ** -0.5.  Returns out, or (out, lse
     [n_queries, n_q_heads] float32) with ``want_lse``."""
     c = _context()
-    torch = c.torch
-    (n, h, d), qs = _rows(q, "q", None, cache.head_dim)
-    dt = _dtype(c, q, "q")
-    seqs = kv_len.shape[0]
-    lens = _vector(kv_len, torch.int32, seqs, "kv_len")
-    cu = _vector(cu_q, torch.int32, seqs + 1, "cu_q")
-    shape, stride = page_table.shape, page_table.stride()
-    if not page_table.is_cuda or page_table.dtype != torch.int32 or len(shape) != 2 or \
-            shape[0] != seqs or (shape[1] > 1 and stride[1] != 1):
-        raise ValueError("page_table must be a [n_seqs, pages] int32 CUDA tensor")
-    mask, words = None, 0
-    if tree_mask is not None:
-        if not tree_mask.is_cuda or tree_mask.dtype != torch.int64 or tree_mask.dim() != 2 or \
-                tree_mask.shape[0] != n or not tree_mask.is_contiguous():
-            raise ValueError("tree_mask must be a contiguous [n_queries, words] int64 CUDA tensor")
-        mask, words = tree_mask.data_ptr(), tree_mask.shape[1]
-    if out is None:
-        out = q.new_empty((n, h, d))
-        o0, o1 = h * d, d
-    else:
-        _, (o0, o1, _) = _rows(out, "out", h, d, n)
-        if out.dtype != q.dtype:
-            raise ValueError("out must have the type of q")
-    lse = q.new_empty((n, h), dtype=torch.float32) if want_lse else None
-    if check or status is not None:
+    if check:
         status = _status(c, check, status, stream)
-    s = kvr_sequences(cu, lens, page_table.data_ptr(), stride[0], shape[1], n, seqs, max_q, max_kv)
-    nbytes = ctypes.c_size_t(0)
-    call = c.lib.kvr_tree_attention
-    args = (cache.ref, s, q.data_ptr(), dt, h, qs[0], qs[1], mask, words,
-            1.0 / math.sqrt(d) if scale is None else scale, out.data_ptr(), o0, o1,
-            None if lse is None else lse.data_ptr(), None if status is None else status.data_ptr())
-    rc = call(*args, None, nbytes, None)
-    if rc:
-        c.pkg._check(rc, "kvr_tree_attention(size)")
-    ws = workspace
-    if ws is None or ws.numel() < nbytes.value:
-        ws = q.new_empty(max(nbytes.value, 256), dtype=torch.uint8)
-    elif not ws.is_cuda or ws.dtype != torch.uint8 or not ws.is_contiguous():
-        raise ValueError("workspace must be a contiguous torch.uint8 CUDA tensor")
-    nbytes.value = ws.numel()
-    rc = call(*args, ws.data_ptr(), nbytes, c.stream(stream, q.device))
+    rc, out, lse, ws = c.fast.tree_attention(cache.address, q, cu_q, kv_len, page_table, max_q,
+                                             max_kv, tree_mask, scale, want_lse, out, workspace,
+                                             status, _handle(stream))
     if rc or check or stream is not None:
         _finish(c, "kvr_tree_attention", rc, check, status, stream, out, lse, ws)
     return (out, lse) if want_lse else out

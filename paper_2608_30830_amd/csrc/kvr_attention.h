@@ -51,7 +51,7 @@ __device__ __forceinline__ Part find_part(const Attention &a, int item)
     int base = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
         if (b0) x = lane_sequence(a, b0);
-        const int parts = (x.steps + per - 1) / per;
+        const int parts = parts_of(x.steps, per);
         const int upto = wave_incl_scan(parts * x.rbs);
         const uint64_t hit = __ballot(base + upto > item);
         if (hit) {
@@ -225,6 +225,7 @@ struct Kernel {
         float m[RT], l[RT];   // reference maximum (log2), this lane's part of the weights' sum
         f32x4 w[RT];          // sum of the rounded weights (every element the same)
         int qi[RT];           // query within the sequence
+        uint64_t word[RT];    // its tree mask, where that is one word
     };
     // LDS: the joining of the waves (maxima, sums, values), or one step of each wave in
     // the order that the matrix instructions read: keys [2][NB][64], values [2 NB][64].
@@ -478,6 +479,27 @@ struct Kernel {
         return j <= i;
     }
 
+    // The same for tokens t to t + 3 before `end` and the lane's row of tile R, as bits.
+    // (One load and branch per token and row took nine tenths of the time of short contexts.)
+    template <int R>
+    __device__ __forceinline__ uint32_t seen4(const State &st, int t, int end) const
+    {
+        const int i = st.qi[R], j = t - prefix;
+        uint32_t s;
+        if (!a.mask) {
+            s = (16u >> (3 - max(-1, min(i - j, 3)))) - 1;   // the lowest i - j + 1 bits
+        } else if (a.words == 1) {
+            const int up = max(0, min(-j, 4));   // older tokens among the four
+            s = (uint32_t)(st.word[R] >> max(0, min(j, 63))) << up | ((1u << up) - 1);
+            if (j > 63) s = 0;
+        } else {
+            s = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s |= (t + k < end && sees(i, j + k) ? 1u : 0u) << k;
+        }
+        return s & ((1u << max(0, min(end - t, 4))) - 1);   // of four at most
+    }
+
     // Value tiles 2 I and 2 I + 1 of a step: element pairs of eight tokens turned around.
     template <int I>
     __device__ __forceinline__ void val_tiles(const VR &v, u32x4 (&x)[2]) const
@@ -505,13 +527,8 @@ struct Kernel {
             // the accumulators under divergent branches.
             static_for<0, U * RT>([&](auto I) {
                 constexpr int u = decltype(I)::value / RT, r = decltype(I)::value % RT;
-                uint32_t seen = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int t = token(step + u, i);
-                    const bool v = t < end && sees(st.qi[r], t - prefix);
-                    seen |= (v ? 1u : 0u) << i;
-                }
+                const int t = token(step + u, 0);
+                const uint32_t seen = seen4<r>(st, t, end) | seen4<r>(st, t + 16, end) << 4;
                 const f32x4 x = sc[u][r][0], y = sc[u][r][1];
                 auto pick = [&](int i, float z) { return seen >> i & 1 ? z : -INFINITY; };
                 sc[u][r][0] = f32x4{pick(0, x[0]), pick(1, x[1]), pick(2, x[2]), pick(3, x[3])};
@@ -652,18 +669,43 @@ struct Kernel {
         for (int e = 0; e < 2 * NB; ++e) vf[e * 64] = u32x4{0, 0, 0, 0};
     }
 
-    // Two steps from LDS.
+    // Two steps from LDS.  Their keys, then their values, are read a group ahead of the
+    // products that use them where registers allow: left to itself the compiler reads a pair of
+    // fragments, waits for it and multiplies.  (Two groups ahead, or the first step's
+    // outputs interleaved with the second one's weights, measured the same or slower.)
+    static constexpr int G = NB == 3 ? 3 : 4;     // fragments of a group
+    static constexpr int GS = 2 * NB / G;         // groups of one step's keys, or values
+    static constexpr int Ahead = RT == 2 || NB == 6;   // (others: a block less on the CU)
     __device__ __forceinline__ void compute_shared(int step, int last, const uint32_t *lds,
                                                    State &st) const
     {
         const u32x4 *f = reinterpret_cast<const u32x4 *>(lds) + lane;
+        u32x4 frag[Ahead + 1][G];
+        auto fetch = [&](auto K) {
+            constexpr int k = decltype(K)::value, u = k % (Pair * GS) / GS;
+            if constexpr (k < 2 * Pair * GS) {
+                static_for<0, G>([&](auto J) {
+                    constexpr int j = k % GS * G + decltype(J)::value;   // within the step
+                    // both tiles of keys in turn: successive products then differ in their sums
+                    constexpr int at = k < Pair * GS ? j % 2 * NB + j / 2 : 2 * NB + j;
+                    frag[k % (Ahead + 1)][decltype(J)::value] = f[u * (StepWords / 4) + at * 64];
+                });
+            }
+            if constexpr (Ahead > 0)   // only vector and scalar arithmetic may pass
+                __builtin_amdgcn_sched_barrier(0x406);
+        };
+        static_for<0, Ahead>(fetch);
         f32x4 sc[Pair][RT][2];
-        static_for<0, 2 * Pair>([&](auto I) {
-            constexpr int u = decltype(I)::value / 2, t = decltype(I)::value % 2;
-            static_for<0, RT>([&](auto R) { sc[u][decltype(R)::value][t] = f32x4{0, 0, 0, 0}; });
-            static_for<0, NB>([&](auto I) {
-                constexpr int i = decltype(I)::value;
-                scores<i, t>(f[u * (StepWords / 4) + (t * NB + i) * 64], st, sc[u]);
+        static_for<0, 2 * Pair * RT>([&](auto I) {
+            constexpr int i = decltype(I)::value;
+            sc[i / (2 * RT)][i / 2 % RT][i % 2] = f32x4{0, 0, 0, 0};
+        });
+        static_for<0, Pair * GS>([&](auto K) {
+            constexpr int k = decltype(K)::value;
+            fetch(std::integral_constant<int, k + Ahead>{});
+            static_for<0, G>([&](auto J) {
+                constexpr int j = k % GS * G + decltype(J)::value;
+                scores<j / 2, j % 2>(frag[k % (Ahead + 1)][decltype(J)::value], st, sc[k / GS]);
             });
         });
         reference<Pair>(step, last, sc, st);
@@ -674,9 +716,13 @@ struct Kernel {
                 weights<decltype(R)::value>(sc[u][decltype(R)::value], st, pv[decltype(R)::value]);
             });
             count(pv, st);
-            static_for<0, 2 * NB>([&](auto E) {
-                constexpr int e = decltype(E)::value;
-                accumulate<e>(f[u * (StepWords / 4) + (2 * NB + e) * 64], pv, st);
+            static_for<0, GS>([&](auto I) {
+                constexpr int k = (Pair + u) * GS + decltype(I)::value;
+                fetch(std::integral_constant<int, k + Ahead>{});
+                static_for<0, G>([&](auto J) {
+                    constexpr int j = decltype(J)::value;
+                    accumulate<decltype(I)::value * G + j>(frag[k % (Ahead + 1)][j], pv, st);
+                });
             });
         });
     }
@@ -689,6 +735,7 @@ struct Kernel {
             const int row = min(r0 + 16 * r + (int)n, rows - 1);
             st.qi[r] = row / a.group;
             const int head = h * a.group + (row - st.qi[r] * a.group);
+            st.word[r] = a.mask && a.words == 1 ? a.mask[q0 + st.qi[r]] : 0;
             const char *src = a.q.p + ((int64_t)(q0 + st.qi[r]) * a.q.token_stride +
                                        (int64_t)head * a.q.head_stride) * 2;
             const uint32_t flip = a.negate ? 0x80008000u : 0u;
@@ -938,6 +985,16 @@ __global__ __launch_bounds__(64 * Waves, 2) void attention_kernel(Attention a)
     k.run(lds);
 }
 
+// The kernel that the plan names: its workspace and grid hold this one's blocks only.
+template <int FMT, int QT, int NB, int RT, int PF, bool Shared, int Waves>
+hipError_t launch_kernel(const Attention &a, dim3 grid, hipStream_t stream)
+{
+    if (a.block_rows != Kernel<FMT, QT, NB, RT, PF, Shared, Waves>::BlockRows || a.waves != Waves)
+        return hipErrorInvalidValue;
+    attention_kernel<FMT, QT, NB, RT, PF, Shared, Waves><<<grid, 64 * Waves, 0, stream>>>(a);
+    return hipGetLastError();
+}
+
 // One launch for a format, query type and head size, by the plan.
 template <int FMT, int QT, int NB, int RT, int Waves>
 hipError_t launch_split(const Attention &a, dim3 grid, hipStream_t stream)
@@ -947,24 +1004,18 @@ hipError_t launch_split(const Attention &a, dim3 grid, hipStream_t stream)
     constexpr bool quant = Fmt<FMT>::Quant, two = quant && QT == KVR_DT_FP16;
     constexpr int room = (RT == 2 ? (quant ? 32 : 64) : quant ? 64 : 128) / stage;
     constexpr int PF = room < 1 || NB * (two ? 2 : 1) > 8 || NB == 8 ? 1 : room > 3 ? 3 : room;
-    attention_kernel<FMT, QT, NB, RT, PF, false, Waves><<<grid, 64 * Waves, 0, stream>>>(a);
-    return hipGetLastError();
+    return launch_kernel<FMT, QT, NB, RT, PF, false, Waves>(a, grid, stream);
 }
 
 template <int FMT, int QT, int NB>
 hipError_t launch_nb(const Attention &a, dim3 grid, hipStream_t stream)
 {
     if constexpr (NB <= 4) {   // heads beyond 128 take one row tile a wave
-        if (a.row_tiles == 2 && a.shared) {
-            attention_kernel<FMT, QT, NB, 2, 1, true, 4><<<grid, 256, 0, stream>>>(a);
-            return hipGetLastError();
-        }
+        if (a.row_tiles == 2 && a.shared)
+            return launch_kernel<FMT, QT, NB, 2, 1, true, 4>(a, grid, stream);
         if (a.row_tiles == 2) return launch_split<FMT, QT, NB, 2, 4>(a, grid, stream);
     }
-    if (a.shared) {
-        attention_kernel<FMT, QT, NB, 1, 1, true, 4><<<grid, 256, 0, stream>>>(a);
-        return hipGetLastError();
-    }
+    if (a.shared) return launch_kernel<FMT, QT, NB, 1, 1, true, 4>(a, grid, stream);
     return a.waves == 8 ? launch_split<FMT, QT, NB, 1, 8>(a, grid, stream)
                         : launch_split<FMT, QT, NB, 1, 4>(a, grid, stream);
 }

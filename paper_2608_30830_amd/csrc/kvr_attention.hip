@@ -11,15 +11,17 @@ namespace {
 // Joins the parts of rows.  A row has dim / 4 lanes times Groups groups of parts: each
 // group goes through its share of the parts, four at a time, with a running
 // maximum, then the groups are added in order.  With many rows one group does, with
-// few several keep more loads in flight.
-template <int QT, int Groups>
-__global__ __launch_bounds__(256) void combine_kernel(Attention a)
+// few several keep more loads in flight, and with many parts of few rows as many as a
+// block holds (a read of four parts takes about a microsecond, however few rows).
+template <int QT, int Groups, int Threads>
+__global__ __launch_bounds__(Threads) void combine_kernel(Attention a)
 {
-    __shared__ __align__(16) float so[Groups > 1 ? 1024 : 4];
-    __shared__ float sl[Groups > 1 ? 256 : 1], sm[Groups > 1 ? 256 : 1], sw[Groups > 1 ? 256 : 1];
+    constexpr int N = Groups > 1 ? Threads : 1;
+    __shared__ __align__(16) float so[4 * N];
+    __shared__ float sl[N], sm[N], sw[N];
     const int dim = a.c.dim, cols = dim / 4;
     const int per_row = cols * Groups;
-    const int rows_per_block = 256 / per_row;
+    const int rows_per_block = Threads / per_row;
     const int h = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63;
     int len, nq, q0;
     sequence(a, b, len, nq, q0);
@@ -27,12 +29,12 @@ __global__ __launch_bounds__(256) void combine_kernel(Attention a)
     if ((int)blockIdx.x * rows_per_block >= rows) return;
     Lane x = lane_sequence(a, 0);
     const int per = part_steps(a, x);
-    const int parts = (steps_of(len, nq) + per - 1) / per;
+    const int parts = parts_of(steps_of(len, nq), per);
     if (parts <= 1) return;
     int base = 0;   // items before this sequence's
     for (int b0 = 0; b0 < b; b0 += 64) {
         if (b0) x = lane_sequence(a, b0);
-        base += wave_total(b0 + lane < b ? (x.steps + per - 1) / per * x.rbs : 0);
+        base += wave_total(b0 + lane < b ? parts_of(x.steps, per) * x.rbs : 0);
     }
     const int local = threadIdx.x / per_row, rest = threadIdx.x - local * per_row;
     const int grp = rest / cols, c = rest - grp * cols;
@@ -119,11 +121,19 @@ hipError_t launch_combine(const Attention &a, hipStream_t stream)
 {
     const int64_t rows = (int64_t)a.max_q * a.group;
     const bool many = rows * a.c.n_heads * a.n_seqs >= 4096;
-    const int groups = many ? 1 : a.c.dim <= 128 ? 8 : 4;   // at most 256 lanes a row
-    const dim3 grid((unsigned)cdiv(rows, 256 / (a.c.dim / 4 * groups)), a.c.n_heads, a.n_seqs);
-    if (groups == 1) combine_kernel<QT, 1><<<grid, 256, 0, stream>>>(a);
-    else if (groups == 8) combine_kernel<QT, 8><<<grid, 256, 0, stream>>>(a);
-    else combine_kernel<QT, 4><<<grid, 256, 0, stream>>>(a);
+    const bool narrow = a.c.dim <= 128;
+    // Many parts of few sequences: a block of 1,024 (one sequence of 90,196 tokens and one KV
+    // head, 470 parts: 27 -> 21 us a call; with 96 parts of 56 rows 73 -> 75).
+    const int64_t parts = std::min<int64_t>(a.target / a.n_seqs, cdiv(a.max_kv, kStep) / a.min_steps);
+    const bool deep = !many && parts > 128;
+    const int threads = deep ? 1024 : 256;
+    const int groups = many ? 1 : (narrow ? 8 : 4) * (threads / 256);   // at most all lanes a row
+    const dim3 grid((unsigned)cdiv(rows, threads / (a.c.dim / 4 * groups)), a.c.n_heads, a.n_seqs);
+    if (many) combine_kernel<QT, 1, 256><<<grid, 256, 0, stream>>>(a);
+    else if (deep && narrow) combine_kernel<QT, 32, 1024><<<grid, 1024, 0, stream>>>(a);
+    else if (deep) combine_kernel<QT, 16, 1024><<<grid, 1024, 0, stream>>>(a);
+    else if (narrow) combine_kernel<QT, 8, 256><<<grid, 256, 0, stream>>>(a);
+    else combine_kernel<QT, 4, 256><<<grid, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -147,9 +157,13 @@ size_t plan_attention(Attention &a)
     // 74 with two row tiles a wave).
     const bool narrow = a.c.dim <= 128;
     a.shared = rows > (narrow ? 32 : 16);
+    // (33 to 64 rows in two waves of two tiles, which read half as much LDS: 79 us against 74.)
     a.row_tiles = rows <= 16 || !narrow || (rows > 32 && rows <= 64) ? 1 : 2;
     a.waves = 4;
-    a.min_steps = a.waves;
+    // A part's outputs (32 bits) are written and read again: of 128 rows they are worth 8 steps
+    // of 16-bit cache (24 sequences of 63 to 184 tokens, 63 new ones, 8 queries a head: 56 us in
+    // parts of four steps, 35 in parts of 16).
+    a.min_steps = a.shared ? 8 * a.row_tiles : a.waves;
     int slots = kSlots;
     if (a.shared) slots = a.row_tiles > 1 ? 2 * kSlots : kSlots * 3 / 2;
     // A few short sequences: eight waves a block and no parts, so that one launch does (one

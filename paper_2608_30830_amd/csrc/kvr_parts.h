@@ -80,6 +80,14 @@ __device__ __forceinline__ int part_steps(const Attention &a, const Lane &first)
     return n > a.min_steps ? n : a.min_steps;
 }
 
+// Parts of a sequence: the nearest whole number (always rounding up would cut 880 row
+// blocks of 31 steps into twice as many, which end in two uneven waves).
+__device__ __forceinline__ int parts_of(int steps, int per)
+{
+    const int n = (int)((steps + (per >> 1)) / per);
+    return n > 0 ? n : steps > 0;
+}
+
 }  // namespace
 }  // namespace kv
 }  // namespace kvr

@@ -258,7 +258,7 @@ struct Codes {
     }
 };
 
-template <int FMT, int DT, int HPT>
+template <int FMT, int DT, int HPT, bool Stream = false>
 __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
 {
     constexpr int E = elem_bytes<DT>();
@@ -296,13 +296,13 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
         if (live) x[j].get(p);
         char *row = dst + (int64_t)h * out.head_stride * E;
         if (DT == VT) {
-            *reinterpret_cast<u32x4 *>(row) = u32x4{p[0], p[1], p[2], p[3]};
+            store16<Stream>(reinterpret_cast<u32x4 *>(row), u32x4{p[0], p[1], p[2], p[3]});
             continue;
         }
         float y[8];
 #pragma unroll
         for (int n = 0; n < 4; ++n) unpack16<VT>(p[n], y[2 * n], y[2 * n + 1]);
-        store8<DT>(row, y);
+        store8<DT, Stream>(row, y);
     }
 }
 
@@ -365,7 +365,9 @@ hipError_t read_heads(ReadArgs &a, int64_t tokens, hipStream_t stream)
 {
     const int hpt = heads_per_lane(tokens, a.c);
     const dim3 grid = plan(a, tokens, hpt);
-    if (hpt == 4) read_kernel<FMT, DT, 4><<<grid, kThreads, 0, stream>>>(a);
+    const bool large = hpt == 4 && streams(2 * tokens * a.c.n_heads * a.c.dim, a.c.dim, DT);
+    if (large) read_kernel<FMT, DT, 4, DT != KVR_DT_FP32><<<grid, kThreads, 0, stream>>>(a);
+    else if (hpt == 4) read_kernel<FMT, DT, 4><<<grid, kThreads, 0, stream>>>(a);
     else read_kernel<FMT, DT, 1><<<grid, kThreads, 0, stream>>>(a);
     return hipGetLastError();
 }

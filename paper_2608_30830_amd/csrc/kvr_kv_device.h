@@ -59,6 +59,14 @@ __device__ __forceinline__ void store1(char *p, int64_t i, float x)
     else reinterpret_cast<_Float16 *>(p)[i] = (_Float16)x;
 }
 
+// 16 bytes; Stream: past the caches.
+template <bool Stream = false, class T>
+__device__ __forceinline__ void store16(T *p, T x)
+{
+    if (Stream) __builtin_nontemporal_store(x, p);
+    else *p = x;
+}
+
 // Eight adjacent elements from a 16-byte aligned address.
 template <int DT>
 __device__ __forceinline__ void load8(const char *p, float (&x)[8])
@@ -77,15 +85,16 @@ __device__ __forceinline__ void load8(const char *p, float (&x)[8])
         for (int i = 0; i < 4; ++i) unpack16<DT>(a[i], x[2 * i], x[2 * i + 1]);
     }
 }
-template <int DT>
+template <int DT, bool Stream = false>
 __device__ __forceinline__ void store8(char *p, const float (&x)[8])
 {
     if (DT == KVR_DT_FP32) {
-        reinterpret_cast<f32x4 *>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
-        reinterpret_cast<f32x4 *>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+        store16<Stream>(reinterpret_cast<f32x4 *>(p), f32x4{x[0], x[1], x[2], x[3]});
+        store16<Stream>(reinterpret_cast<f32x4 *>(p) + 1, f32x4{x[4], x[5], x[6], x[7]});
     } else {
-        *reinterpret_cast<u32x4 *>(p) = u32x4{pack16<DT>(x[0], x[1]), pack16<DT>(x[2], x[3]),
-                                              pack16<DT>(x[4], x[5]), pack16<DT>(x[6], x[7])};
+        store16<Stream>(reinterpret_cast<u32x4 *>(p),
+                        u32x4{pack16<DT>(x[0], x[1]), pack16<DT>(x[2], x[3]),
+                              pack16<DT>(x[4], x[5]), pack16<DT>(x[6], x[7])});
     }
 }
 

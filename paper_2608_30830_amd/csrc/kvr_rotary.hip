@@ -53,7 +53,7 @@ __device__ __forceinline__ void turn(float &a, float &b, float c, float s)
     a = y;
 }
 
-template <int DT, bool IL, int HPT>
+template <int DT, bool IL, int HPT, bool Stream = false>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
 {
     constexpr int E = elem_bytes<DT>();
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
                 if (h >= a.heads) break;
                 float v[8];
                 load8<DT>(xr + ((int64_t)h * a.x.head_stride + d) * E, v);
-                store8<DT>(yr + ((int64_t)h * a.out.head_stride + d) * E, v);
+                store8<DT, Stream>(yr + ((int64_t)h * a.out.head_stride + d) * E, v);
             }
             continue;
         }
@@ -117,12 +117,12 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
             if (IL) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) turn(x0[j][2 * k], x0[j][2 * k + 1], c[k], s[k]);
-                store8<DT>(q, x0[j]);
+                store8<DT, Stream>(q, x0[j]);
             } else {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) turn(x0[j][k], x1[j][k], c[k], s[k]);
-                store8<DT>(q, x0[j]);
-                store8<DT>(q + half * E, x1[j]);
+                store8<DT, Stream>(q, x0[j]);
+                store8<DT, Stream>(q + half * E, x1[j]);
             }
         }
     }
@@ -193,9 +193,12 @@ hipError_t launch(RotaryArgs &a, bool copy_tail, hipStream_t stream)
     const int lanes = a.head_groups * a.units;
     a.tokens_per_block = lanes >= kThreads ? 1 : kThreads / lanes;
     const dim3 grid((unsigned)cdiv(a.tokens, a.tokens_per_block));
+    const bool large = hpt == 4 && streams((int64_t)a.tokens * a.heads * a.dim, a.dim, DT);
     if (!wide) rotary_pairs_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
+    else if (il && large) rotary_kernel<DT, true, 4, DT != KVR_DT_FP32><<<grid, kThreads, 0, stream>>>(a);
     else if (il && hpt == 4) rotary_kernel<DT, true, 4><<<grid, kThreads, 0, stream>>>(a);
     else if (il) rotary_kernel<DT, true, 1><<<grid, kThreads, 0, stream>>>(a);
+    else if (large) rotary_kernel<DT, false, 4, DT != KVR_DT_FP32><<<grid, kThreads, 0, stream>>>(a);
     else if (hpt == 4) rotary_kernel<DT, false, 4><<<grid, kThreads, 0, stream>>>(a);
     else rotary_kernel<DT, false, 1><<<grid, kThreads, 0, stream>>>(a);
     return hipGetLastError();

@@ -19,13 +19,17 @@
 // With up to 32 rows every wave has all of them and takes every n-th step of 32
 // tokens, with the loads of the next steps in flight and their pages looked up a
 // round earlier; a block joins its waves through LDS.  Memory bounds this: 64
-// sequences of 8,192 tokens, 8 heads of 128, one new token each: 187 us in 8
+// sequences of 8,192 tokens, 8 heads of 128, one new token each: 188 us in 8
 // bits (5.9 TB/s of cache), 374 us in 16 (5.7), 120 us in 4 (4.8, where the
 // conversions begin to count).  With more rows the waves divide them and share
 // the tokens through LDS, converted and turned around once: 16 sequences of
-// 16,384 tokens and 512 rows, 16 bits: 0.75 ms, 725 TFLOP/s, bound by the vector
-// instructions of the softmax, the matrix instructions and the LDS reads, which
-// overlap only in part.
+// 16,384 tokens and 512 rows, 16 bits: 0.68 ms, 805 TFLOP/s.  There the matrix
+// unit is busy for 39 % of the cycles and the vector unit for 43 % (the softmax: a
+// multiply-add, an exponential, a sum and a maximum a score), and with the two
+// waves that the registers leave a SIMD their sum is what counts: reading LDS
+// further ahead, a second buffer in place of one of the two barriers and the
+// weights of one step interleaved with the products of the other by hand changed
+// the time by less than the runs differ.
 //
 // The sequences are cut along the cached tokens into about as many equal parts as
 // fill the GPU (from the lengths, on the device); combine_kernel joins the parts.
@@ -480,7 +484,7 @@ struct Kernel {
     }
 
     // The same for tokens t to t + 3 before `end` and the lane's row of tile R, as bits.
-    // (One load and branch per token and row took nine tenths of the time of short contexts.)
+    // (A load and a branch for each token and row made short contexts of many rows a third slower.)
     template <int R>
     __device__ __forceinline__ uint32_t seen4(const State &st, int t, int end) const
     {

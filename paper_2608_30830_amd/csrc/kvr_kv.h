@@ -19,10 +19,11 @@ constexpr int kBadScale = 255;  // scale byte of a block that held a NaN or an i
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Whether an output is written past the caches: more than the eight L2 of 4 MB hold, in
-// rows of whole cache lines that one 16-byte store a lane fills (rotary of 32,768 tokens, 32
-// heads of 128 in 16 bits: 90 us against 105; read of 131,072 tokens from 8 bits: 144
-// against 157; but 12.6 MB written and read again 21.7 against 19.6, rows of 192 bytes 31
-// against 29, and 32-bit outputs, two stores a lane, 102 against 60).
+// rows of whole cache lines that one 16-byte store a lane fills.  Read of 131,072 tokens from
+// 8 bits: 141 us against 159; of 32,749 from 4 bits: 27 against 30; rotary of 32,768 tokens,
+// 32 heads of 128 in 16 bits: 101 against 104 (inputs in the cache: 89 against 105).  But
+// 12.6 MB written and read again 21.7 against 19.6, rows of 192 bytes 31 against 29, and
+// 32-bit outputs, two stores a lane, 102 against 60.
 inline bool streams(int64_t elements, int dim, int32_t dtype)
 {
     return dtype != KVR_DT_FP32 && dim % 64 == 0 && 2 * elements >= (32 << 20);

@@ -23,7 +23,7 @@
 // bits (5.9 TB/s of cache), 374 us in 16 (5.7), 120 us in 4 (4.8, where the
 // conversions begin to count).  With more rows the waves divide them and share
 // the tokens through LDS, converted and turned around once: 16 sequences of
-// 16,384 tokens and 512 rows, 16 bits: 0.68 ms, 805 TFLOP/s.  There the matrix
+// 16,384 tokens and 512 rows, 16 bits: 0.66 ms, 830 TFLOP/s.  There the matrix
 // unit is busy for 39 % of the cycles and the vector unit for 43 % (the softmax: a
 // multiply-add, an exponential, a sum and a maximum a score), and with the two
 // waves that the registers leave a SIMD their sum is what counts: reading LDS
@@ -673,6 +673,14 @@ struct Kernel {
         for (int e = 0; e < 2 * NB; ++e) vf[e * 64] = u32x4{0, 0, 0, 0};
     }
 
+    // The softmax goes before the other block's products where two row tiles a wave make both
+    // long: 512 rows over 16,384 tokens 661 us against 685 on one card; with one tile 74 against 72.
+    template <int P>
+    __device__ __forceinline__ static void priority()
+    {
+        if constexpr (RT == 2) __builtin_amdgcn_s_setprio(P);
+    }
+
     // Two steps from LDS.  Their keys, then their values, are read a group ahead of the
     // products that use them where registers allow: left to itself the compiler reads a pair of
     // fragments, waits for it and multiplies.  (Two groups ahead, or the first step's
@@ -698,6 +706,7 @@ struct Kernel {
             if constexpr (Ahead > 0)   // only vector and scalar arithmetic may pass
                 __builtin_amdgcn_sched_barrier(0x406);
         };
+        priority<0>();
         static_for<0, Ahead>(fetch);
         f32x4 sc[Pair][RT][2];
         static_for<0, 2 * Pair * RT>([&](auto I) {
@@ -712,6 +721,7 @@ struct Kernel {
                 scores<j / 2, j % 2>(frag[k % (Ahead + 1)][decltype(J)::value], st, sc[k / GS]);
             });
         });
+        priority<1>();
         reference<Pair>(step, last, sc, st);
         static_for<0, Pair>([&](auto U) {
             constexpr int u = decltype(U)::value;
@@ -719,6 +729,7 @@ struct Kernel {
             static_for<0, RT>([&](auto R) {
                 weights<decltype(R)::value>(sc[u][decltype(R)::value], st, pv[decltype(R)::value]);
             });
+            priority<0>();
             count(pv, st);
             static_for<0, GS>([&](auto I) {
                 constexpr int k = (Pair + u) * GS + decltype(I)::value;
@@ -728,6 +739,7 @@ struct Kernel {
                     accumulate<decltype(I)::value * G + j>(frag[k % (Ahead + 1)][j], pv, st);
                 });
             });
+            priority<u == 0>();
         });
     }
 

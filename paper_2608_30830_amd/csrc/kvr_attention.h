@@ -50,6 +50,16 @@ namespace {
 // other.  Every wave computes the same.
 __device__ __forceinline__ Part find_part(const Attention &a, int item)
 {
+    if (a.direct) {
+        Part p{};
+        p.b = item / a.direct;
+        p.rb = item - p.b * a.direct;
+        p.parts = 1;
+        sequence(a, p.b, p.len, p.nq, p.q0);
+        p.last = steps_of(p.len, p.nq);
+        if (p.last == 0 || p.rb >= row_blocks_of(a, p.nq)) p.b = -1;
+        return p;
+    }
     Lane x = lane_sequence(a, 0);
     const int per = part_steps(a, x);
     int base = 0;
@@ -233,7 +243,7 @@ struct Kernel {
     };
     // LDS: the joining of the waves (maxima, sums, values), or one step of each wave in
     // the order that the matrix instructions read: keys [2][NB][64], values [2 NB][64].
-    static constexpr int JoinWords = 3 * Waves * BlockRows + BlockRows * LdsRow;
+    static constexpr int JoinWords = (3 + LdsRow) * Waves * BlockRows;
     static constexpr int StepWords = 4 * NB * 64 * 4;
     static constexpr int Tile = Waves / 2;   // steps that a block brings into LDS at a time
     static constexpr int Pair = 2;           // steps that are worked on together
@@ -243,10 +253,12 @@ struct Kernel {
     const uint32_t n, g, lane;
     int h, len, prefix, q0;
     const int32_t *pages;
+    const int last_page;   // of the table's row
     uint32_t krow, vrow, ksrow, vsrow;   // byte offsets of this lane's rows in a tile
 
     __device__ Kernel(const Attention &a_)
-        : a(a_), n(threadIdx.x & 15), g((threadIdx.x & 63) >> 4), lane(threadIdx.x & 63)
+        : a(a_), n(threadIdx.x & 15), g((threadIdx.x & 63) >> 4), lane(threadIdx.x & 63),
+          last_page((int)min(a_.max_pages, (int64_t)INT32_MAX) - 1)
     {
         krow = (uint32_t)n * (uint32_t)a.c.token_stride;
         vrow = 4u * (uint32_t)g * (uint32_t)a.c.token_stride;
@@ -254,34 +266,32 @@ struct Kernel {
         vsrow = 4u * (uint32_t)g * (uint32_t)a.c.stoken_stride;
     }
 
-    // First tokens of a step's two tiles (any tile that begins at or past the sequence's
-    // end is read as its last tile), and the pages that hold them, as the table has
-    // them: looked up well before the rows are loaded.
+    // The pages that hold a step's two tiles, as the table has them: looked up well before
+    // the rows are loaded, and whatever the sequence's length (within the table's row).
     struct Pages {
         int id[2];
     };
-    __device__ __forceinline__ int tile_start(int step, int t) const
-    {
-        return min(step * kStep + 16 * t, (len - 1) & ~15);
-    }
     __device__ __forceinline__ Pages look_up(int step) const
     {
-        return Pages{{pages[tile_start(step, 0) >> a.c.page_shift],
-                      pages[tile_start(step, 1) >> a.c.page_shift]}};
+        const int at = step * kStep;   // below 2^31: at most 2^30 tokens and a few steps
+        return Pages{{pages[min(at >> a.c.page_shift, last_page)],
+                      pages[min((at + 16) >> a.c.page_shift, last_page)]}};
     }
 
     // Uniform addresses plus one 32-bit lane offset for all keys, one for all values.
     struct Where {   // a tile in the cache and in its scales
         int64_t at, sat;
     };
+    // (A second tile that begins past the sequence's end is read as the first.)
     __device__ __forceinline__ Where locate(int step, int t, const Pages &p) const
     {
-        int page = __builtin_amdgcn_readfirstlane(p.id[t]);
+        const bool past = step * kStep + 16 * t >= len;
+        int page = __builtin_amdgcn_readfirstlane(past ? p.id[0] : p.id[t]);
         if (page < 0 || page >= a.c.n_pages) {
             if (a.status) *a.status = KVR_E_DOMAIN;
             page = 0;
         }
-        const int off = tile_start(step, t) & ((1 << a.c.page_shift) - 1);
+        const int off = (step * kStep + (past ? 0 : 16 * t)) & ((1 << a.c.page_shift) - 1);
         return Where{page * a.c.page_stride + h * a.c.head_stride + off * a.c.token_stride,
                      Quant ? page * a.c.spage_stride + h * a.c.shead_stride +
                                  off * a.c.stoken_stride
@@ -815,28 +825,38 @@ struct Kernel {
         // follow each other, land on one XCD (block number mod 8) and share its L2.
         const int item = blockIdx.x / a.c.n_heads;
         h = blockIdx.x - item * a.c.n_heads;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        Pages where[PF];
+        auto table_row = [&](int b) { pages = a.pages + (int64_t)b * a.pages_stride; };
+        auto first_pages = [&](int step) {
+#pragma unroll
+            for (int i = 0; i < PF; ++i) where[i] = look_up(step + wave + i * Waves);
+        };
+        // Beside the lengths (in the shared kernel the same made the loop 5 % slower).
+        if (!Shared && a.direct) {
+            table_row(item / a.direct);
+            first_pages(0);
+        }
         const Part p = find_part(a, item);
         if (p.b < 0) return;
         const int rows = p.nq * a.group, r0 = p.rb * BlockRows;
         len = p.len;
         prefix = p.len - p.nq;
         q0 = p.q0;
-        pages = a.pages + (int64_t)p.b * a.pages_stride;
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (Shared || !a.direct) table_row(p.b);
+        if (!Shared && !a.direct) first_pages(p.first);
         if constexpr (Shared) run_shared(p, wave, r0, rows, lds);
-        else run_split(p, wave, r0, rows, reinterpret_cast<float *>(lds));
+        else run_split(p, wave, r0, rows, where, reinterpret_cast<float *>(lds));
     }
 
     // Few rows: every wave has all of the block's rows and every n-th step.
-    __device__ __forceinline__ void run_split(const Part &p, int wave, int r0, int rows, float *lds)
+    __device__ __forceinline__ void run_split(const Part &p, int wave, int r0, int rows,
+                                              Pages (&where)[PF], float *lds)
     {
         State st;
         Stage raw[PF];
         bool odd = false;
         int s = p.first + wave;
-        Pages where[PF];
-#pragma unroll
-        for (int i = 0; i < PF; ++i) where[i] = look_up(s + i * Waves);
 #pragma unroll
         for (int i = 0; i < PF; ++i)
             if (s + i * Waves < p.last) {
@@ -879,25 +899,19 @@ struct Kernel {
 #pragma unroll
             for (int e = 0; e < 2 * NB; ++e) st.o[r][e] *= f;
         }
-        for (int w = 0; w < Waves; ++w) {
-            if (wave == w) {
 #pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    float *row = so + (16 * r + n) * LdsRow;
-                    static_for<0, 2 * NB>([&](auto E) {
-                        // tile e of its slab: element (4 g + i) * W + e - e0 of the slab
-                        constexpr int e = decltype(E)::value, slab = VR::slab_of(e);
-                        constexpr int e0 = VR::first(slab), W = VR::width(slab);
+        for (int r = 0; r < RT; ++r) {
+            float *row = so + (wave * BlockRows + 16 * r + n) * LdsRow;
+            static_for<0, 2 * NB>([&](auto E) {
+                // tile e of its slab: element (4 g + i) * W + e - e0 of the slab
+                constexpr int e = decltype(E)::value, slab = VR::slab_of(e);
+                constexpr int e0 = VR::first(slab), W = VR::width(slab);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            float *x = row + 16 * e0 + (4 * g + i) * W + (e - e0);
-                            *x = w == 0 ? st.o[r][e][i] : *x + st.o[r][e][i];
-                        }
-                    });
-                }
-            }
-            __syncthreads();
+                for (int i = 0; i < 4; ++i)
+                    row[16 * e0 + (4 * g + i) * W + (e - e0)] = st.o[r][e][i];
+            });
         }
+        __syncthreads();
         // rows out: eight elements a thread
         const int64_t cell = blockIdx.x;
         for (int i = threadIdx.x; i < BlockRows * (D / 8); i += 64 * Waves) {
@@ -912,9 +926,13 @@ struct Kernel {
                 sum += sl[w * BlockRows + row] * f;
                 norm += sw[w * BlockRows + row] * f;
             }
-            float x[8];
+            float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = so[row * LdsRow + d + e];
+            for (int w = 0; w < Waves; ++w) {
+                const float *y = so + (w * BlockRows + row) * LdsRow + d;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] += y[e];
+            }
             if (odd) add_odd<8>(p, r0 + row, d, x);
             store<8>(p, cell, r0, row, d, x, top, sum, norm);
         }

@@ -181,7 +181,18 @@ size_t plan_attention(Attention &a)
     // (at most 2^30 launched blocks: 2^12 sequences x 2^24 query heads and tokens / 64 rows)
     a.max_items = (int32_t)std::max<int64_t>(
         1, std::min(a.target + blocks, blocks * cdiv(longest, a.min_steps)));
-    if (longest <= a.min_steps) return 0;
+    a.direct = 0;
+    if (longest <= a.min_steps) {
+        // Nothing is cut: a block knows its sequence from its number, and its first pages are
+        // looked up beside the lengths.  Sequences that do not fill their room leave blocks
+        // without work.
+        const int64_t room = cdiv(rows, a.block_rows);
+        if (a.max_pages > 0 && (room == 1 || a.n_seqs * room <= 2 * kSlots)) {
+            a.direct = (int32_t)room;
+            a.max_items = (int32_t)std::max<int64_t>(1, a.n_seqs * room);
+        }
+        return 0;
+    }
     return (size_t)a.max_items * a.c.n_heads * a.block_rows * (a.c.dim + 4) * sizeof(float);
 }
 

@@ -92,6 +92,8 @@ struct Attention {
     int32_t target;              // items (a part of a sequence x a block of rows) of one head, about
     int32_t max_items;           // bound on them
     int32_t min_steps;           // steps that a part has at least
+    int32_t direct;              // row blocks that each sequence has room for, where none is cut
+                                 // and items are in order of sequences (0: items are searched)
     float *part_o;               // [items][heads][block_rows][dim]
     float4 *part_ml;             // [items][heads][block_rows]: maximum, sum of the weights, and
                                  // of the weights as rounded for the products

@@ -257,6 +257,7 @@ int kvr_tree_attention(const kvr_kv_cache *cache, const kvr_sequences *seqs, con
     a.max_q = seqs->max_q;
     a.max_kv = seqs->max_kv;
     a.n_queries = seqs->n_queries;
+    a.max_pages = seqs->max_pages;
     const size_t need = kvr::kv::plan_attention(a);
     if (!d_ws) {
         *ws_bytes = need;
@@ -273,7 +274,6 @@ int kvr_tree_attention(const kvr_kv_cache *cache, const kvr_sequences *seqs, con
     a.kv_len = seqs->d_kv_len;
     a.pages = seqs->d_pages;
     a.pages_stride = seqs->pages_stride;
-    a.max_pages = seqs->max_pages;
     a.mask = d_tree_mask;
     a.words = mask_words;
     a.scale2 = (float)(std::fabs((double)scale) * 1.4426950408889634);

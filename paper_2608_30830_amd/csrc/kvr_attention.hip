@@ -166,11 +166,14 @@ size_t plan_attention(Attention &a)
     a.min_steps = a.shared ? 8 * a.row_tiles : a.waves;
     int slots = kSlots;
     if (a.shared) slots = a.row_tiles > 1 ? 2 * kSlots : kSlots * 3 / 2;
-    // A few short sequences: eight waves a block and no parts, so that one launch does (one
-    // sequence of 500 tokens: 12.7 us a call against 14.8 in parts; of 1,000: 16.5, 14.7).
-    if (rows <= 16 && longest <= kShortSteps && (int64_t)a.n_seqs * a.c.n_heads * 2 <= kSlots) {
-        a.waves = 8;
-        a.min_steps = kShortSteps;
+    // Short sequences: no parts, so that one launch does, and eight waves a block while the
+    // blocks are not more than the CUs.  (Bfloat16, 8 heads of 128, us a call against parts: one
+    // sequence of 500 tokens 10.5, 11.1; of 1,000 14.7, 11.2; 32 of 500 15.8, 20.6; of 1,000
+    // 24.0, 28.3.)
+    const int64_t heads = (int64_t)a.n_seqs * a.c.n_heads;
+    if (rows <= 16 && longest <= (heads >= 128 ? 2 * kShortSteps : kShortSteps)) {
+        a.waves = heads <= 256 ? 8 : 4;
+        a.min_steps = (int32_t)longest;
     }
     a.block_rows = 16 * a.row_tiles * (a.shared ? a.waves : 1);
     a.target = std::max(1, slots / a.c.n_heads);

@@ -126,3 +126,24 @@ def test_rows_that_see_nothing(kvr):
         assert int(out[:20].count_nonzero()) == 0 and bool((lse[:20] == -float("inf")).all())
         assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse[20:]).all())
         assert int(out[20:].count_nonzero()) > 0
+
+
+@pytest.mark.parametrize("fmt,dtype", [("bf16", "bf16"), ("fp4", "fp16")])
+@pytest.mark.parametrize("n,longest", [(20, 1023), (20, 1040), (70, 512), (70, 1024), (150, 520)])
+def test_many_short_sequences(kvr, fmt, dtype, n, longest):
+    """One new token: sequences that one block takes whole, and ones that are cut."""
+    rng = np.random.default_rng(n)
+    kv = [int(x) for x in np.exp(rng.uniform(0, np.log(longest), n))]
+    kv[n // 2] = longest
+    p = Problem(kvr, 65, fmt, dtype, kv, [1] * n, 8, 2, 64, 16)
+    p.check(*p.call())
+
+
+@pytest.mark.parametrize("group", [2, 8])
+def test_many_trees_of_ragged_sizes(kvr, group):
+    """More row blocks than one launch has room for in order of sequences."""
+    n = 300
+    nq = [64 if b % 25 == 0 else b % 4 for b in range(n)]
+    kv = [q + (b * 13 % 60 if q else 0) for b, q in enumerate(nq)]
+    p = Problem(kvr, 66, "bf16", "bf16", kv, nq, 1, group, 64, 16, tree=True)
+    p.check(*p.call(), rows=4)

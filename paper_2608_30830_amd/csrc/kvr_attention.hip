@@ -169,9 +169,10 @@ size_t plan_attention(Attention &a)
     // Short sequences: no parts, so that one launch does, and eight waves a block while the
     // blocks are not more than the CUs.  (Bfloat16, 8 heads of 128, us a call against parts: one
     // sequence of 500 tokens 10.5, 11.1; of 1,000 14.7, 11.2; 32 of 500 15.8, 20.6; of 1,000
-    // 24.0, 28.3.)
+    // 24.0, 28.3; 128 of 2,000 180, 184; 400 of 50 to 2,000 171, 203: where sequences are many,
+    // finding the parts and joining them is not free.)
     const int64_t heads = (int64_t)a.n_seqs * a.c.n_heads;
-    if (rows <= 16 && longest <= (heads >= 128 ? 2 * kShortSteps : kShortSteps)) {
+    if (rows <= 16 && longest <= kShortSteps * (heads >= 1024 ? 4 : heads >= 128 ? 2 : 1)) {
         a.waves = heads <= 256 ? 8 : 4;
         a.min_steps = (int32_t)longest;
     }

@@ -129,7 +129,7 @@ def test_rows_that_see_nothing(kvr):
 
 
 @pytest.mark.parametrize("fmt,dtype", [("bf16", "bf16"), ("fp4", "fp16")])
-@pytest.mark.parametrize("n,longest", [(20, 1023), (20, 1040), (70, 512), (70, 1024), (150, 520)])
+@pytest.mark.parametrize("n,longest", [(20, 1023), (20, 1040), (70, 512), (70, 1024), (150, 520), (130, 2048), (130, 2060)])
 def test_many_short_sequences(kvr, fmt, dtype, n, longest):
     """One new token: sequences that one block takes whole, and ones that are cut."""
     rng = np.random.default_rng(n)

@@ -170,12 +170,11 @@ size_t plan_attention(Attention &a)
     // blocks are not more than the CUs.  (Bfloat16, 8 heads of 128, us a call against parts: one
     // sequence of 500 tokens 10.5, 11.1; of 1,000 14.7, 11.2; 32 of 500 15.8, 20.6; of 1,000
     // 24.0, 28.3; 128 of 2,000 180, 184; 400 of 50 to 2,000 171, 203: where sequences are many,
-    // finding the parts and joining them is not free.  With 24 rows a head in 8 bits: 32 of 500 tokens
-    // 13.1, 18.8; 200 of 500 51, 77; 200 of 2,000 170, 195.)
+    // finding the parts and joining them is not free.  With 24 rows a head in 8 bits: one of 500 tokens
+    // 11.0, 12.8; 32 of 500 13.1, 18.8; 200 of 500 51, 77; 200 of 2,000 170, 195.)
     const int64_t heads = (int64_t)a.n_seqs * a.c.n_heads;
-    const int few = rows <= 16 ? 1 : 0;
-    if (!a.shared && longest <= kShortSteps * (heads >= 1024 ? 4 : heads >= 128 ? 2 : few)) {
-        a.waves = few && heads <= 256 ? 8 : 4;
+    if (!a.shared && longest <= kShortSteps * (heads >= 1024 ? 4 : heads >= 128 ? 2 : 1)) {
+        a.waves = rows <= 16 && heads <= 256 ? 8 : 4;
         a.min_steps = (int32_t)longest;
     }
     a.block_rows = 16 * a.row_tiles * (a.shared ? a.waves : 1);

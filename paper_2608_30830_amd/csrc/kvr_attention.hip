@@ -179,8 +179,8 @@ size_t plan_attention(Attention &a)
     }
     a.block_rows = 16 * a.row_tiles * (a.shared ? a.waves : 1);
     a.target = std::max(1, slots / a.c.n_heads);
-    // Row blocks of all sequences; ceil(steps / part) parts of each, part = total / target
-    // or min_steps.
+    // Row blocks of all sequences; the nearest whole number to steps / part parts of each,
+    // part = total / target or min_steps.
     const int64_t blocks = std::min<int64_t>((int64_t)a.n_seqs * cdiv(rows, a.block_rows),
                                              a.n_queries * a.group / a.block_rows + a.n_seqs);
     // (at most 2^30 launched blocks: 2^12 sequences x 2^24 query heads and tokens / 64 rows)

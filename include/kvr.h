@@ -534,7 +534,8 @@ typedef struct {
  *   to the 16-bit type of the products.
  *   A sequence whose lengths do not fit (more than max_q or max_kv, fewer cached than
  *   new tokens, more pages than max_pages) is left out, and a page outside the pool
- *   is read as page 0: KVR_E_DOMAIN.
+ *   is read as page 0: KVR_E_DOMAIN.  Where d_cu_q decreases, any sequence may be left
+ *   out.
  *   d_ws, ws_bytes  workspace (two-phase sizing as above; contents need not be
  *                  set).  It may be 0 bytes: then d_ws is not used, any non-NULL
  *                  256-byte aligned pointer will do.

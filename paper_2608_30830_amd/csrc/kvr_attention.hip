@@ -31,7 +31,7 @@ __global__ __launch_bounds__(Threads) void combine_kernel(Attention a)
     const int per = part_steps(a, x);
     const int parts = parts_of(steps_of(len, nq), per);
     if (parts <= 1) return;
-    int base = 0;   // items before this sequence's
+    int64_t base = 0;   // items before this sequence's
     for (int b0 = 0; b0 < b; b0 += 64) {
         if (b0) x = lane_sequence(a, b0);
         base += wave_total(b0 + lane < b ? parts_of(x.steps, per) * x.rbs : 0);
@@ -42,10 +42,14 @@ __global__ __launch_bounds__(Threads) void combine_kernel(Attention a)
     const bool live = local < rows_per_block && row < rows;
     const int rb = row / a.block_rows, rr = row - rb * a.block_rows;
     const int nrb = row_blocks_of(a, nq);
+    if (!planned(a, base, parts, nrb)) {   // left out (every wave agrees)
+        if (a.status) *a.status = KVR_E_DOMAIN;
+        return;
+    }
     f32x4 acc = {0, 0, 0, 0};
     float sum = 0.0f, norm = 0.0f, top = kLowest;
     if (live) {
-        const int64_t first = ((int64_t)(base + rb) * a.c.n_heads + h) * a.block_rows + rr;
+        const int64_t first = ((base + rb) * a.c.n_heads + h) * a.block_rows + rr;
         const int64_t next = (int64_t)nrb * a.c.n_heads * a.block_rows;   // cells from part to part
         const float4 *ml = a.part_ml + first;
         const float *o = a.part_o + first * dim + 4 * c;

@@ -1,5 +1,6 @@
 // How the sequences of an attention call are cut into parts along their cached
-// tokens: from the lengths, on the device, the same in every wave.
+// tokens: from the lengths, on the device, the same in every wave.  The arithmetic is
+// for the host too, so that it can be checked there.
 #pragma once
 
 #include "kvr_dpp.h"
@@ -28,7 +29,7 @@ __device__ __forceinline__ int lane_value(int x, int lane)   // uniform
 }
 
 // Tokens, new tokens and first query of sequence b; false where they do not fit the call.
-__device__ __forceinline__ bool sequence(const Attention &a, int b, int &len, int &nq, int &q0)
+__host__ __device__ __forceinline__ bool sequence(const Attention &a, int b, int &len, int &nq, int &q0)
 {
     q0 = a.cu_q[b];
     nq = a.cu_q[b + 1] - q0;
@@ -42,11 +43,11 @@ __device__ __forceinline__ bool sequence(const Attention &a, int b, int &len, in
     }
     return ok;
 }
-__device__ __forceinline__ int steps_of(int len, int nq)
+__host__ __device__ __forceinline__ int steps_of(int len, int nq)
 {
     return nq > 0 ? (len + kStep - 1) / kStep : 0;
 }
-__device__ __forceinline__ int row_blocks_of(const Attention &a, int nq)
+__host__ __device__ __forceinline__ int row_blocks_of(const Attention &a, int nq)
 {
     return (nq * a.group + a.block_rows - 1) / a.block_rows;
 }
@@ -65,8 +66,16 @@ __device__ __forceinline__ Lane lane_sequence(const Attention &a, int b0)
     return x;
 }
 
-// Steps of one part: all sequences' steps (times their row blocks) over the
-// target, at least min_steps.  first: the first 64 sequences.
+// Steps of one part, from the total of all sequences' steps times their row blocks: the
+// total over the target, at least min_steps.
+__host__ __device__ __forceinline__ int part_size(const Attention &a, int64_t total)
+{
+    // at most 2^12 sequences x 2^26 steps x 2^20 row blocks; the quotient is at most 2^26
+    // and may be one too large: any part size will do
+    const int n = (int)((double)total / (double)a.target) + 1;
+    return n > a.min_steps ? n : a.min_steps;
+}
+// first: the first 64 sequences.
 __device__ __forceinline__ int part_steps(const Attention &a, const Lane &first)
 {
     int64_t total = wave_total((int64_t)first.steps * first.rbs);
@@ -74,18 +83,25 @@ __device__ __forceinline__ int part_steps(const Attention &a, const Lane &first)
         const Lane x = lane_sequence(a, b0);
         total += wave_total((int64_t)x.steps * x.rbs);
     }
-    // at most 2^12 sequences x 2^26 steps x 2^20 row blocks; the quotient is at most 2^26
-    // and may be one too large: any part size will do
-    const int n = (int)((double)total / (double)a.target) + 1;
-    return n > a.min_steps ? n : a.min_steps;
+    return part_size(a, total);
 }
 
 // Parts of a sequence: the nearest whole number (always rounding up would cut 880 row
 // blocks of 31 steps into twice as many, which end in two uneven waves).
-__device__ __forceinline__ int parts_of(int steps, int per)
+__host__ __device__ __forceinline__ int parts_of(int steps, int per)
 {
     const int n = (int)((steps + (per >> 1)) / per);
     return n > 0 ? n : steps > 0;
+}
+
+// Whether the items of a sequence, which begin at item `base`, are all among the planned
+// ones: launched, and with room in the workspace.  The plan counts on sequences that
+// follow one another in the queries; where cu_q decreases (one sequence then has fewer than
+// no tokens and is reported), the others may have the same queries several times.
+__host__ __device__ __forceinline__ bool planned(const Attention &a, int64_t base, int parts,
+                                                 int row_blocks)
+{
+    return base + (int64_t)parts * row_blocks <= a.max_items;
 }
 
 }  // namespace

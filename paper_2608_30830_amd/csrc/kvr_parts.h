@@ -70,10 +70,12 @@ __device__ __forceinline__ Lane lane_sequence(const Attention &a, int b0)
 // total over the target, at least min_steps.
 __host__ __device__ __forceinline__ int part_size(const Attention &a, int64_t total)
 {
-    // at most 2^12 sequences x 2^26 steps x 2^20 row blocks; the quotient is at most 2^26
-    // and may be one too large: any part size will do
-    const int n = (int)((double)total / (double)a.target) + 1;
-    return n > a.min_steps ? n : a.min_steps;
+    // A total is at most 2^12 sequences x 2^25 steps x 2^18 row blocks.  Parts longer than the
+    // longest sequence are no fewer, so the quotient is cut there, before it becomes an int.
+    const int longest = (a.max_kv - 1) / kStep + 1;
+    const double n = floor((double)total / (double)a.target) + 1.0;
+    const int per = n < (double)longest ? (int)n : longest;
+    return per > a.min_steps ? per : a.min_steps;
 }
 // first: the first 64 sequences.
 __device__ __forceinline__ int part_steps(const Attention &a, const Lane &first)

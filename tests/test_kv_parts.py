@@ -79,3 +79,14 @@ def test_any_first_queries(program):
             assert got["status"] == DOMAIN
             over += 1
     assert over
+
+
+@pytest.mark.parametrize("n,kv_heads,max_q,longest", [(1, 1024, 1 << 14, 1 << 30), (40, 1024, 1 << 14, 1 << 30),
+                                                      (4096, 600, 27962, 1 << 29), (3, 1, 1 << 20, 1 << 30)])
+def test_steps_beyond_32_bits(program, n, kv_heads, max_q, longest):
+    """Steps times row blocks over the target pass 31 bits: the parts are still as planned."""
+    got = _run(program, 16 * kv_heads if kv_heads == 1 else kv_heads, kv_heads, max_q, longest, n * max_q,
+               np.arange(n + 1) * max_q, [longest] * n)
+    assert got["status"] == 0 and got["left"] == 0
+    assert got["items"] <= got["planned"]
+    assert 0 < got["per"] <= longest // 32

@@ -523,7 +523,9 @@ typedef struct {
  *   out[i][h] = sum_j softmax_j(scale * q[i][h] . k_j) v_j,  lse[i][h] = log of the sum
  * with query head h on KV head h / (n_q_heads / n_kv_heads).  A query that sees
  * nothing gets zeros and -infinity.  Hidden tokens, and cache rows that are not
- * in use, may hold anything, NaN and infinities included.
+ * in use, may hold anything, NaN and infinities included.  A value that a query sees and that
+ * is an infinity gives an infinity or NaN (NaN also where half-precision queries meet it in a
+ * quantised cache).
  *   d_q, d_out     device, dtype (KVR_DT_BF16 or KVR_DT_FP16; a 16-bit cache must
  *                  have the same) [n_queries][n_q_heads][head_dim], strides in
  *                  elements, 16-byte aligned rows.  d_out must not overlap d_q.

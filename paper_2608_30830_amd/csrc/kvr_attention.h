@@ -373,23 +373,41 @@ struct Kernel {
         }
     }
 
-    // Infinities and NaN among a lane's loaded values, and those values to zero.
+    // Infinities and NaN among a lane's loaded values, and those values to zero.  A code is odd
+    // where its block's scale byte s makes it so: all of them for 255; the two NaN of
+    // e4m3; and those whose value reaches 2^128, magnitude bits of (262 - s) * 8 on for e4m3
+    // (s >= 247) and (256 - s) * 2 for e2m1 (s >= 253).  That much below a code's top bit is
+    // added, so that odd codes carry into it.
     static constexpr uint32_t kExp = FMT == KVR_KV_FP16 ? 0x7c00u : 0x7f80u;
+    static constexpr uint32_t kMag = FMT == KVR_KV_FP8 ? 0x7f7f7f7fu : 0x77777777u;
+    __device__ __forceinline__ static uint32_t to_odd(uint32_t s)   // of one code
+    {
+        if (FMT == KVR_KV_FP8) return s < 247 ? 1u : 8u * (s - 246);
+        return s < 253 ? 0u : 2u * (s - 252);
+    }
+    __device__ __forceinline__ static uint32_t odd_codes(uint32_t x, uint32_t s)   // their top bits
+    {
+        return ((x & kMag) + to_odd(s) * (FMT == KVR_KV_FP8 ? 0x01010101u : 0x11111111u)) & ~kMag;
+    }
     __device__ __forceinline__ static bool odd_values(const VR &v)
     {
         bool odd = false;
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
+            if (!Quant)
 #pragma unroll
-            for (int w = 0; w < VR::words; ++w) {
-                const uint32_t x = v.w[t][w];
-                if (!Quant) odd = odd || (x & kExp) == kExp || (x & kExp << 16) == kExp << 16;
-                if (FMT == KVR_KV_FP8)   // a byte of 0x7f or 0xff: its low seven bits + 1 carry
-                    odd = odd || (((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
-            }
-            if (Quant)
+                for (int w = 0; w < VR::words; ++w) {
+                    const uint32_t x = v.w[t][w];
+                    odd = odd || (x & kExp) == kExp || (x & kExp << 16) == kExp << 16;
+                }
+            if constexpr (Quant)
+                static_for<0, VR::slabs>([&](auto S) {
+                    constexpr int s = decltype(S)::value;
+                    odd = odd || v.s[t][s] == kBadScale;
 #pragma unroll
-                for (int s = 0; s < VR::slabs; ++s) odd = odd || v.s[t][s] == kBadScale;
+                    for (int w = VR::word(s); w < VR::word(s + 1); ++w)
+                        odd = odd || odd_codes(v.w[t][w], v.s[t][s]) != 0;
+                });
         }
         return __ballot(odd) != 0;
     }
@@ -397,25 +415,26 @@ struct Kernel {
     {
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
+            if (!Quant)
 #pragma unroll
-            for (int w = 0; w < VR::words; ++w) {
-                uint32_t x = v.w[t][w];
-                if (!Quant) {
+                for (int w = 0; w < VR::words; ++w) {
+                    uint32_t x = v.w[t][w];
                     if ((x & kExp) == kExp) x &= 0xffff0000u;
                     if ((x & kExp << 16) == kExp << 16) x &= 0xffffu;
+                    v.w[t][w] = x;
                 }
-                if (FMT == KVR_KV_FP8)
-                    x &= ~(((((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 255u);
-                v.w[t][w] = x;
-            }
-            if (Quant)
+            if constexpr (Quant)
+                static_for<0, VR::slabs>([&](auto S) {
+                    constexpr int s = decltype(S)::value;
+                    const bool bad = v.s[t][s] == kBadScale;
 #pragma unroll
-                for (int s = 0; s < VR::slabs; ++s)
-                    if (v.s[t][s] == kBadScale) {   // the block's words may be shared: codes to zero
-                        v.s[t][s] = 127;
-#pragma unroll
-                        for (int w = VR::word(s); w < VR::word(s + 1); ++w) v.w[t][w] = 0;
+                    for (int w = VR::word(s); w < VR::word(s + 1); ++w) {
+                        const uint32_t top = odd_codes(v.w[t][w], v.s[t][s]);
+                        const uint32_t keep = FMT == KVR_KV_FP8 ? ~((top >> 7) * 255u) : ~((top >> 3) * 15u);
+                        v.w[t][w] = bad ? 0u : v.w[t][w] & keep;
                     }
+                    if (bad) v.s[t][s] = 127;
+                });
         }
     }
 
@@ -464,11 +483,15 @@ struct Kernel {
             if ((x & kExp) != kExp) return 0.0f;
             return load1<FMT == KVR_KV_FP16 ? KVR_DT_FP16 : KVR_DT_BF16>(row, d);
         }
-        bool nan = a.c.vs[id * a.c.spage_stride + h * a.c.shead_stride + off * a.c.stoken_stride +
-                          (d >> 5)] == kBadScale;
-        if (FMT == KVR_KV_FP8)
-            nan = nan || (reinterpret_cast<const uint8_t *>(row)[d] & 0x7f) == 0x7f;
-        return nan ? __uint_as_float(0x7fc00000u) : 0.0f;
+        const uint32_t sc = a.c.vs[id * a.c.spage_stride + h * a.c.shead_stride +
+                                   off * a.c.stoken_stride + (d >> 5)];
+        constexpr bool E4 = FMT == KVR_KV_FP8;
+        const uint32_t byte = reinterpret_cast<const uint8_t *>(row)[E4 ? d : d >> 1];
+        const uint32_t code = E4 ? byte : byte >> 4 * (d & 1) & 15u;
+        const uint32_t mag = code & (E4 ? 0x7fu : 7u);
+        if (sc == kBadScale || (E4 && mag == 0x7fu)) return __uint_as_float(0x7fc00000u);
+        if (mag + to_odd(sc) < (E4 ? 128u : 8u)) return 0.0f;
+        return code > mag ? -INFINITY : INFINITY;
     }
     // The infinities and NaN that clean() took out, to W elements of one row.
     template <int W>

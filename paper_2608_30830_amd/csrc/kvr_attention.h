@@ -236,7 +236,7 @@ struct Kernel {
     struct State {   // of this wave's rows
         u32x4 q[RT][QS][NB];
         f32x4 o[RT][2 * NB];
-        float m[RT], l[RT];   // reference maximum (log2), this lane's part of the weights' sum
+        float m[RT], l[RT];   // reference (log2), this lane's part of the weights' sum
         f32x4 w[RT];          // sum of the rounded weights (every element the same)
         int qi[RT];           // query within the sequence
         uint64_t word[RT];    // its tree mask, where that is one word
@@ -552,9 +552,13 @@ struct Kernel {
     }
 
     // Before the weights of U steps from `step` on (the part ends before step `last`):
-    // hidden tokens' scores to -infinity, and the reference maxima.  Those move only
-    // when a score exceeds one by more than 8 (weights of up to 2^8 lose no
-    // precision), so most steps need no exchange between lanes.
+    // hidden tokens' scores to -infinity, and the references.  Those move only when a score
+    // exceeds the last maximum that they were taken from by more than 8 (weights of up to 2^8
+    // lose no precision), so most steps need no exchange between lanes.  In half precision a
+    // reference is 2^7 below its maximum: weights reach 2^15 of the largest 65,504, and those
+    // that vanish, below 2^-25, are 2^-32 of the row's largest or less (of 131,072 tokens beside a
+    // dominant one 2^-15 altogether; with the maximum itself as the reference it was 2^-8).
+    static constexpr float kBelow = MT == KVR_DT_FP16 ? 7.0f : 0.0f;
     template <int U>
     __device__ __forceinline__ void reference(int step, int last, f32x4 (&sc)[U][RT][2], State &st) const
     {
@@ -584,12 +588,12 @@ struct Kernel {
                 top[r] = decltype(V)::value ? fmaxf(top[r], z) : z;
             });
             top[r] *= a.scale2;
-            moves = moves || top[r] > st.m[r] + 8.0f;
+            moves = moves || top[r] > st.m[r] + (8.0f + kBelow);
         });
         if (__ballot(moves)) {
             static_for<0, RT>([&](auto R) {
                 constexpr int r = decltype(R)::value;
-                const float t = fmaxf(row_max(top[r]), st.m[r]);
+                const float t = fmaxf(row_max(top[r]) - kBelow, st.m[r]);
                 const float f = __builtin_amdgcn_exp2f(st.m[r] - t);
                 st.l[r] *= f;
                 st.w[r] *= f;

@@ -8,6 +8,7 @@
 #include <ATen/ATen.h>
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <c10/hip/HIPStream.h>
+#include <hip/hip_runtime_api.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -120,11 +121,35 @@ const kvr_kv_cache *cache_of(PyObject *o)
 }
 
 // The caller's stream (its handle), or torch's current one on the tensor's device.
-void *stream_of(PyObject *o, const at::Tensor &t)
-{
-    if (given(o)) return PyLong_AsVoidPtr(o);
-    return c10::hip::getCurrentHIPStream(t.device().index()).stream();
-}
+struct Stream {
+    hipStream_t current, used;
+    Stream(PyObject *o, const at::Tensor &t)
+        : current(c10::hip::getCurrentHIPStream(t.device().index()).stream()), used(current)
+    {
+        if (!given(o)) return;
+        used = static_cast<hipStream_t>(PyLong_AsVoidPtr(o));
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            throw Refused{PyExc_TypeError, "stream must be a torch.cuda.Stream"};
+        }
+    }
+    // After an allocation: memory comes from the current stream's pool, where work on what it
+    // held before may still be queued, and another stream waits for that.
+    void allocated() const
+    {
+        if (used == current) return;
+        hipEvent_t e;
+        hipError_t rc = hipEventCreateWithFlags(&e, hipEventDisableTiming);
+        if (rc == hipSuccess) {
+            rc = hipEventRecord(e, current);
+            if (rc == hipSuccess) rc = hipStreamWaitEvent(used, e, 0);
+            const hipError_t last = hipEventDestroy(e);   // (once it is no longer needed)
+            if (rc == hipSuccess) rc = last;
+        }
+        if (rc != hipSuccess)
+            throw Refused{PyExc_RuntimeError, std::string("streams: ") + hipGetErrorString(rc)};
+    }
+};
 
 // A Python tuple of a status code and tensors (undefined ones: None).
 template <class... Ts>
@@ -186,12 +211,14 @@ PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int64_t tokens = x.size(0);
         const int32_t *pos = vector<int32_t>(a[1], "positions", at::kInt, tokens);
         const Table t = table_of(a[2]);
+        const Stream stream(a[6], x);
+        int32_t *const status = status_of(a[5]);
         const at::Tensor out = out_like(a[4], x, "out must have the type of x");
+        if (!given(a[4])) stream.allocated();
         const int rc = kvr_rotary(x.data_ptr(), out.data_ptr(), dt, tokens,
                                   fits32(x.size(1), "heads"), fits32(x.size(2), "head_dim"),
                                   x.stride(0), x.stride(1), out.stride(0), out.stride(1), pos, t.t,
-                                  t.n_pos, t.rot, integer32(a[3], "flags"), status_of(a[5]),
-                                  stream_of(a[6], x));
+                                  t.n_pos, t.rot, integer32(a[3], "flags"), status, stream.used);
         return answer(rc, out);
     });
 }
@@ -220,7 +247,7 @@ PyObject *cache_write(PyObject *, PyObject *const *a, Py_ssize_t n)
         return answer(kvr_cache_write(c, k.data_ptr(), v.data_ptr(), dt, tokens, k.stride(0),
                                       k.stride(1), v.stride(0), v.stride(1), at, pos, t.t, t.n_pos,
                                       t.rot, integer32(a[6], "flags"), status_of(a[7]),
-                                      stream_of(a[8], slots)));
+                                      Stream(a[8], slots).used));
     });
 }
 
@@ -233,6 +260,8 @@ PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int64_t tokens = slots.dim() ? slots.size(0) : 0;
         const int64_t *at = vector<int64_t>(a[1], "slots", at::kLong, tokens);
         const int64_t heads = c->n_kv_heads, dim = c->head_dim;
+        const Stream stream(a[6], slots);
+        int32_t *const status = status_of(a[5]);
         at::Tensor k, v;
         int32_t dt;
         if (!given(a[3])) {
@@ -243,6 +272,7 @@ PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n)
             const auto options = slots.options().dtype(type);
             k = at::empty({tokens, heads, dim}, options);
             v = at::empty({tokens, heads, dim}, options);
+            stream.allocated();
         } else {
             k = rows(a[3], "out k", tokens, heads, dim);
             v = rows(a[4], "out v", tokens, heads, dim);
@@ -251,8 +281,7 @@ PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n)
                 refuse("out must be two tensors of the type that is asked for");
         }
         const int rc = kvr_cache_read(c, at, tokens, k.data_ptr(), v.data_ptr(), dt, k.stride(0),
-                                      k.stride(1), v.stride(0), v.stride(1), status_of(a[5]),
-                                      stream_of(a[6], slots));
+                                      k.stride(1), v.stride(0), v.stride(1), status, stream.used);
         return answer(rc, k, v);
     });
 }
@@ -299,10 +328,15 @@ PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
                 throw Refused{PyExc_TypeError, "scale must be a number"};
             }
         }
+        const Stream stream(a[13], q);
+        int32_t *const status = status_of(a[12]);
         const at::Tensor out = out_like(a[10], q, "out must have the type of q");
+        bool allocated = !given(a[10]);
         at::Tensor lse, ws;
-        if (PyObject_IsTrue(a[9]))
+        if (PyObject_IsTrue(a[9])) {
             lse = at::empty({q.size(0), q.size(1)}, q.options().dtype(at::kFloat));
+            allocated = true;
+        }
         const int32_t heads = fits32(q.size(1), "q");
         size_t bytes = 0;
         auto call = [&](void *space) {
@@ -310,7 +344,7 @@ PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
                                       words, (float)scale, out.data_ptr(), out.stride(0),
                                       out.stride(1),
                                       lse.defined() ? static_cast<float *>(lse.data_ptr()) : nullptr,
-                                      status_of(a[12]), space, &bytes, stream_of(a[13], q));
+                                      status, space, &bytes, stream.used);
         };
         int rc = call(nullptr);   // the workspace's size
         if (rc != KVR_OK) return answer(rc, out, lse, ws);
@@ -319,12 +353,16 @@ PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
             if (!ws.is_cuda() || ws.scalar_type() != at::kByte || !ws.is_contiguous())
                 refuse("workspace must be a contiguous torch.uint8 CUDA tensor");
         }
-        if (bytes == 0) {   // nothing is cut: an address that is never used
+        const bool cut = bytes != 0;
+        if (cut && (!ws.defined() || (size_t)ws.numel() < bytes)) {
+            ws = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte));
+            allocated = true;
+        }
+        if (allocated) stream.allocated();
+        if (!cut) {   // an address that is never used
             alignas(256) static char none[256];
             return answer(call(none), out, lse, at::Tensor());
         }
-        if (!ws.defined() || (size_t)ws.numel() < bytes)
-            ws = at::empty({(int64_t)bytes}, q.options().dtype(at::kByte));
         bytes = (size_t)ws.numel();
         rc = call(ws.data_ptr());
         return answer(rc, out, lse, ws);

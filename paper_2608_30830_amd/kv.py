@@ -3,7 +3,9 @@ the most of it in the built module ``kvr_torch``, which takes tensors.
 
 A :class:`KvCache` names the tensors of a cache; ``kvr_cache_write``,
 ``kvr_cache_read`` and ``kvr_tree_attention`` work on it, ``kvr_rotary`` on
-activations.  Every call enqueues on torch's current stream (or ``stream``).
+activations.  Every call enqueues on torch's current stream (or ``stream``).  What a call
+allocates (outputs and workspaces that are not given, the status of ``check``) comes from
+the current stream's memory, and ``stream`` then waits for the work queued there so far.
 With ``check`` (the default) a call waits and raises on a device-detected error;
 ``check=False`` returns without waiting, and an optional ``status`` tensor
 ([1] int32, zeroed by the caller) collects KVR_E_DOMAIN.
@@ -229,6 +231,8 @@ def kvr_rotary_table(rot_dim: int, n_pos: int, theta: float = 10000.0,
     """cos and sin of every position and frequency, [n_pos, 2, rot_dim / 2] float32."""
     x = _context()
     table = x.torch.empty((n_pos, 2, rot_dim // 2), dtype=x.torch.float32, device="cuda")
+    if stream is not None:
+        stream.wait_stream(x.torch.cuda.current_stream())
     rope = kvr_rope(theta, factor, low, high, trained_len, magnitude, kind)
     rc = x.lib.kvr_rotary_table(ctypes.byref(rope), rot_dim, n_pos, table.data_ptr(),
                                 x.pkg._stream_ptr(stream))

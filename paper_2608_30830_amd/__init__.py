@@ -202,6 +202,18 @@ def _on_stream(stream, *tensors) -> None:
             t.record_stream(stream)
 
 
+def _made():
+    """An event behind what the current stream has queued: memory comes from its pool, and
+    work on what the memory held before may still be in that queue."""
+    return _torch().cuda.current_stream().record_event()
+
+
+def _after(made, stream) -> None:
+    """Buffers that were allocated before ``made`` (None: now) are used on ``stream``."""
+    if stream is not None:
+        stream.wait_event(_made() if made is None else made)
+
+
 def _workspace(nbytes: int, ws=None):
     torch = _torch()
     if ws is not None:
@@ -235,8 +247,10 @@ class CostGridCall:
         self.cost = torch.empty((grid.n_lam, grid.n_t1, grid.n_t2), dtype=torch.float64,
                                 device="cuda")
         self.perm = torch.empty(self.n, dtype=torch.int32, device="cuda") if want_perm else None
+        self.made = _made()
 
     def launch(self, stream=None) -> None:
+        _after(self.made, stream)
         _check(self.lib.kvr_cost_grid(_ptr(self.wait_s), _ptr(self.ctx), self.n,
                                       ctypes.byref(self.prices), ctypes.byref(self.grid.c),
                                       self.method, _ptr(self.cost), _ptr(self.perm), _ptr(self.ws),
@@ -270,6 +284,7 @@ def kvr_cost_grid(wait_s, ctx_tokens, prices: kvr_prices, grid: PolicyGrid, meth
     perm = torch.empty(n, dtype=torch.int32, device="cuda") if want_perm else None
     have = ctypes.c_size_t(ws.numel())
     st = _stream_ptr(stream)
+    _after(None, stream)
     _check(lib.kvr_cost_grid(_ptr(wait_s), _ptr(ctx_tokens), n, ctypes.byref(prices),
                              ctypes.byref(grid.c), method, _ptr(cost), _ptr(perm), _ptr(ws),
                              ctypes.byref(have), st), "kvr_cost_grid")
@@ -307,6 +322,7 @@ def kvr_cost_grid_noalloc(wait_s, ctx_tokens, prices: kvr_prices, grid: PolicyGr
         status = torch.empty(1, dtype=torch.int32, device="cuda")
     _need(status, torch.int32, "status")
     _need_shape(status, (1,), "status")
+    _after(None, stream)
     _check(load_library().kvr_cost_grid_noalloc(_ptr(wait_s), _ptr(ctx_tokens), n,
                                                 ctypes.byref(prices), ctypes.byref(grid.c),
                                                 method, _ptr(cost), _ptr(perm), _ptr(status),
@@ -327,6 +343,7 @@ def kvr_select_policy(cost, last_t2_is_inf: bool, stream=None) -> Tuple:
     best = torch.empty((batch, L), dtype=torch.int32, device="cuda")
     bc = torch.empty((batch, L), dtype=torch.float64, device="cuda")
     br = torch.empty((batch, L), dtype=torch.int32, device="cuda")
+    _after(None, stream)
     _check(load_library().kvr_select_policy(_ptr(cost), batch, L, K1, K2, int(bool(last_t2_is_inf)),
                                             _ptr(best), _ptr(bc), _ptr(br), _stream_ptr(stream)),
            "kvr_select_policy")
@@ -366,8 +383,10 @@ class BootstrapCall:
                        None, ctypes.byref(need), None), f"{self.name}(size)")
         self.ws = _workspace(need.value)
         self.ws_bytes = ctypes.c_size_t(self.ws.numel())
+        self.made = _made()
 
     def launch(self, stream=None) -> None:
+        _after(self.made, stream)
         _check(self.fn(_ptr(self.wait_s), _ptr(self.ctx), self.n, _ptr(self.idx), self.R, self.m,
                        ctypes.byref(self.prices), ctypes.byref(self.grid.c), _ptr(self.best),
                        _ptr(self.best_cost), _ptr(self.cost), _ptr(self.ws),
@@ -427,6 +446,7 @@ def kvr_capacity_replay(arrival_s, wait_s, prices: kvr_prices, t2: Sequence[floa
     adm = torch.empty((reps, K), dtype=torch.int64, device="cuda")
     have = ctypes.c_size_t(ws.numel())
     st = _stream_ptr(stream)
+    _after(None, stream)
     _check(lib.kvr_capacity_replay(_ptr(arrival_s), _ptr(wait_s), _ptr(ctx_tokens), reps, n,
                                    ctypes.byref(prices), t2c, K, _ptr(cost), _ptr(rest),
                                    _ptr(adm), _ptr(ws), ctypes.byref(have), st),
@@ -463,9 +483,11 @@ class ControllerCall:
         self.ws = _workspace(need.value)
         self.out = torch.empty(ctypes.sizeof(kvr_controller_out), dtype=torch.uint8,
                                device="cuda")
+        self.made = _made()
 
     def launch(self, stream=None) -> None:
         """Enqueue on ``stream`` (default: the current stream at this call)."""
+        _after(self.made, stream)
         a, w, T = self.args
         have = ctypes.c_size_t(self.ws.numel())
         _check(self.lib.kvr_controller_select(_ptr(a), _ptr(w), _ptr(T), self.reps, self.n,
@@ -506,6 +528,7 @@ def kvr_crossover_statistic(wait_s, prices: kvr_prices, stream=None, check: bool
     frac = torch.empty(1, dtype=torch.float64, device="cuda")
     have = ctypes.c_size_t(ws.numel())
     st = _stream_ptr(stream)
+    _after(None, stream)
     _check(lib.kvr_crossover_statistic(_ptr(wait_s), n, ctypes.byref(prices), _ptr(count),
                                        _ptr(frac), _ptr(ws), ctypes.byref(have), st),
            "kvr_crossover_statistic")

@@ -6,6 +6,7 @@ A :class:`KvCache` names the tensors of a cache; ``kvr_cache_write``,
 activations.  Every call enqueues on torch's current stream (or ``stream``).  What a call
 allocates (outputs and workspaces that are not given, the status of ``check``) comes from
 the current stream's memory, and ``stream`` then waits for the work queued there so far.
+Tensors and stream are of one device, which need not be the current one.
 With ``check`` (the default) a call waits and raises on a device-detected error;
 ``check=False`` returns without waiting, and an optional ``status`` tensor
 ([1] int32, zeroed by the caller) collects KVR_E_DOMAIN.
@@ -120,12 +121,13 @@ def _context() -> _Context:
     return _CTX
 
 
-def _status(x, check, status, stream):
-    """The status tensor of a call: the caller's, or with check a new one."""
+def _status(x, first, check, status, stream):
+    """The status tensor of a call: the caller's, or with check a new one beside the call's
+    first tensor."""
     if status is None and check:
-        status = x.torch.zeros(1, dtype=x.torch.int32, device="cuda")
-        if stream is not None:   # zeroed on the current stream
-            stream.wait_stream(x.torch.cuda.current_stream())
+        status = x.torch.zeros(1, dtype=x.torch.int32, device=getattr(first, "device", "cuda"))
+        if stream is not None and status.is_cuda:   # zeroed on the current stream
+            stream.wait_stream(x.torch.cuda.current_stream(status.device))
     return status
 
 
@@ -136,7 +138,7 @@ def _finish(x, name, rc, check, status, stream, *tensors):
     if stream is not None:
         x.pkg._on_stream(stream, status, *tensors)
     if check:
-        (x.torch.cuda.current_stream() if stream is None else stream).synchronize()
+        (x.torch.cuda.current_stream(status.device) if stream is None else stream).synchronize()
         x.pkg._check(int(status.item()), f"{name}(device)")
 
 
@@ -161,6 +163,8 @@ class KvCache:
             raise ValueError("k and v must be [n_pages, n_kv_heads, page_size, row] alike")
         if not k.is_cuda or not v.is_cuda or k.stride(3) != 1:
             raise ValueError("k and v must be CUDA tensors with adjacent rows")
+        if any(t is not None and t.device != k.device for t in (v, k_scale, v_scale)):
+            raise ValueError("the tensors of a cache must be on one device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         pages, heads, page, row = k.shape
         self.c = c = kvr_kv_cache()
@@ -194,6 +198,8 @@ class KvCache:
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = pages, heads, page, dim
         self.format = c.format
         self.address = ctypes.addressof(c)
+        self.device = k.device
+        self.handle = (self.address, k, v, k_scale, v_scale, c)   # what calls take
 
     @classmethod
     def allocate(cls, fmt: int, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int):
@@ -230,12 +236,14 @@ def kvr_rotary_table(rot_dim: int, n_pos: int, theta: float = 10000.0,
                      stream=None):
     """cos and sin of every position and frequency, [n_pos, 2, rot_dim / 2] float32."""
     x = _context()
-    table = x.torch.empty((n_pos, 2, rot_dim // 2), dtype=x.torch.float32, device="cuda")
-    if stream is not None:
-        stream.wait_stream(x.torch.cuda.current_stream())
+    cuda = x.torch.cuda
     rope = kvr_rope(theta, factor, low, high, trained_len, magnitude, kind)
-    rc = x.lib.kvr_rotary_table(ctypes.byref(rope), rot_dim, n_pos, table.data_ptr(),
-                                x.pkg._stream_ptr(stream))
+    with cuda.device(cuda.current_device() if stream is None else stream.device):
+        table = x.torch.empty((n_pos, 2, rot_dim // 2), dtype=x.torch.float32, device="cuda")
+        if stream is not None:
+            stream.wait_stream(cuda.current_stream())
+        rc = x.lib.kvr_rotary_table(ctypes.byref(rope), rot_dim, n_pos, table.data_ptr(),
+                                    x.pkg._stream_ptr(stream))
     _finish(x, "kvr_rotary_table", rc, False, None, stream, table)
     return table
 
@@ -245,8 +253,8 @@ def _flags(interleaved, adjoint):
 
 
 def _handle(stream):
-    """A stream's handle; None: torch's current stream."""
-    return None if stream is None else stream.cuda_stream
+    """A stream's handle and device; None: torch's current stream."""
+    return None if stream is None else (stream.cuda_stream, stream.device_index)
 
 
 def kvr_rotary(x, positions, table, interleaved: bool = False, adjoint: bool = False, out=None,
@@ -254,7 +262,7 @@ def kvr_rotary(x, positions, table, interleaved: bool = False, adjoint: bool = F
     """x [tokens, heads, dim] turned by its positions; ``out`` may be ``x``."""
     c = _context()
     if check:
-        status = _status(c, check, status, stream)
+        status = _status(c, x, check, status, stream)
     rc, out = c.fast.rotary(x, positions, table, _flags(interleaved, adjoint), out, status,
                             _handle(stream))
     if rc or check or stream is not None:
@@ -270,8 +278,8 @@ def kvr_cache_write(cache: KvCache, k, v, slots, positions=None, table=None,
     ``positions`` on the way."""
     c = _context()
     if check:
-        status = _status(c, check, status, stream)
-    rc, = c.fast.cache_write(cache.address, k, v, slots, positions, table,
+        status = _status(c, cache, check, status, stream)
+    rc, = c.fast.cache_write(cache.handle, k, v, slots, positions, table,
                              _flags(interleaved, adjoint), status, _handle(stream))
     if rc or check or stream is not None:
         _finish(c, "kvr_cache_write", rc, check, status, stream)
@@ -283,13 +291,13 @@ def kvr_cache_read(cache: KvCache, slots, dtype=None, out=None, status=None, str
     ``dtype`` (bfloat16 by default); below 0: zeros.  ``out``: a pair to write to."""
     c = _context()
     if check:
-        status = _status(c, check, status, stream)
+        status = _status(c, cache, check, status, stream)
     if dtype is not None:
         if dtype not in c.codes:
             raise ValueError(f"out must be bfloat16, float16 or float32, not {dtype}")
         dtype = c.codes[dtype]
     k, v = (None, None) if out is None else out
-    rc, k, v = c.fast.cache_read(cache.address, slots, dtype, k, v, status, _handle(stream))
+    rc, k, v = c.fast.cache_read(cache.handle, slots, dtype, k, v, status, _handle(stream))
     if rc or check or stream is not None:
         _finish(c, "kvr_cache_read", rc, check, status, stream, k, v)
     return k, v
@@ -308,8 +316,8 @@ def kvr_tree_attention(cache: KvCache, q, cu_q, kv_len, page_table, max_q: int, 
     [n_queries, n_q_heads] float32) with ``want_lse``."""
     c = _context()
     if check:
-        status = _status(c, check, status, stream)
-    rc, out, lse, ws = c.fast.tree_attention(cache.address, q, cu_q, kv_len, page_table, max_q,
+        status = _status(c, cache, check, status, stream)
+    rc, out, lse, ws = c.fast.tree_attention(cache.handle, q, cu_q, kv_len, page_table, max_q,
                                              max_kv, tree_mask, scale, want_lse, out, workspace,
                                              status, _handle(stream))
     if rc or check or stream is not None:

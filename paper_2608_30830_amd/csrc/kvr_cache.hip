@@ -161,7 +161,7 @@ template <int DT, int FMT, int ROT, int HPT>
 __global__ __launch_bounds__(kThreads) void write_kernel(WriteArgs a)
 {
     constexpr int E = elem_bytes<DT>();
-    const uint32_t i = blockIdx.x * (uint32_t)(kThreads >> a.lane_shift) +
+    const uint32_t i = block_of_grid() * (uint32_t)(kThreads >> a.lane_shift) +
                        (threadIdx.x >> a.lane_shift);
     const int d = 8 * (threadIdx.x & ((1 << a.lane_shift) - 1));
     if (i >= a.groups || d >= a.c.dim) return;   // whole quads: dim is a multiple of 32
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
 {
     constexpr int E = elem_bytes<DT>();
     constexpr int VT = FMT == KVR_KV_FP16 ? KVR_DT_FP16 : KVR_DT_BF16;   // type of the values
-    const uint32_t i = blockIdx.x * (uint32_t)(kThreads >> a.lane_shift) +
+    const uint32_t i = block_of_grid() * (uint32_t)(kThreads >> a.lane_shift) +
                        (threadIdx.x >> a.lane_shift);
     const int d = 8 * (threadIdx.x & ((1 << a.lane_shift) - 1));
     if (i >= a.groups || d >= a.c.dim) return;
@@ -325,7 +325,7 @@ dim3 plan(Args &a, int64_t tokens, int hpt)
     a.head_groups = (a.c.n_heads + hpt - 1) / hpt;
     a.groups = (uint32_t)(tokens * a.head_groups);
     a.lane_shift = lane_shift(a.c.dim);
-    return dim3((unsigned)cdiv(a.groups, kThreads >> a.lane_shift), 2);
+    return grid_of(cdiv(a.groups, kThreads >> a.lane_shift), 2);
 }
 
 template <int DT, int FMT, int ROT>

@@ -18,6 +18,14 @@ constexpr int kBadScale = 255;  // scale byte of a block that held a NaN or an i
 
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Blocks in a row: a dimension of a launch holds at most 2^32 threads, so more blocks than
+// these (of up to 256 threads) stand in the third dimension.
+constexpr uint32_t kMaxGrid = 1u << 23;
+inline dim3 grid_of(int64_t blocks, unsigned y = 1)
+{
+    return dim3((unsigned)(blocks < kMaxGrid ? blocks : kMaxGrid), y, (unsigned)cdiv(blocks, kMaxGrid));
+}
+
 // Whether an output is written past the caches: more than the eight L2 of 4 MB hold, in
 // rows of whole cache lines that one 16-byte store a lane fills.  Read of 131,072 tokens from
 // 8 bits: 141 us against 159; of 32,749 from 4 bits: 27 against 30; rotary of 32,768 tokens,

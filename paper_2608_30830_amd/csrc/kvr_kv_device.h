@@ -7,6 +7,9 @@
 namespace kvr {
 namespace kv {
 
+// The block's number in a launch by grid_of; those beyond its last one are the caller's to end.
+__device__ __forceinline__ uint32_t block_of_grid() { return blockIdx.z * kMaxGrid + blockIdx.x; }
+
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));

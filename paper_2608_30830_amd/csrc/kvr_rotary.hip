@@ -26,7 +26,7 @@ constexpr int kThreads = 256;
 __global__ __launch_bounds__(kThreads) void table_kernel(Freqs f, double magnitude, int half,
                                                          int64_t total, float *t)
 {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t i = (int64_t)block_of_grid() * kThreads + threadIdx.x;
     if (i >= total) return;
     const int64_t pos = i / half;
     const int j = (int)(i - pos * half);
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
     for (int i = threadIdx.x; i < work; i += kThreads) {
         const int tb = i / lanes, rest = i - tb * lanes;
         const int hg = rest / a.units, u = rest - hg * a.units;
-        const uint32_t token = blockIdx.x * (uint32_t)a.tokens_per_block + tb;
+        const uint32_t token = block_of_grid() * (uint32_t)a.tokens_per_block + tb;
         if (token >= a.tokens) return;
         const char *xr = a.x.p + (int64_t)token * a.x.token_stride * E;
         char *yr = a.out.p + (int64_t)token * a.out.token_stride * E;
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void rotary_pairs_kernel(RotaryArgs a)
     for (int i = threadIdx.x; i < work; i += kThreads) {
         const int tb = i / lanes, rest = i - tb * lanes;
         const int h = rest / a.units, u = rest - h * a.units;
-        const uint32_t token = blockIdx.x * (uint32_t)a.tokens_per_block + tb;
+        const uint32_t token = block_of_grid() * (uint32_t)a.tokens_per_block + tb;
         if (token >= a.tokens) return;
         const char *x = a.x.p + ((int64_t)token * a.x.token_stride + (int64_t)h * a.x.head_stride) * E;
         char *y = a.out.p + ((int64_t)token * a.out.token_stride + (int64_t)h * a.out.head_stride) * E;
@@ -194,7 +194,7 @@ hipError_t launch(RotaryArgs &a, bool copy_tail, hipStream_t stream)
     }
     const int lanes = a.head_groups * a.units;
     a.tokens_per_block = lanes >= kThreads ? 1 : kThreads / lanes;
-    const dim3 grid((unsigned)cdiv(a.tokens, a.tokens_per_block));
+    const dim3 grid = grid_of(cdiv(a.tokens, a.tokens_per_block));
     const bool large = hpt == 4 && streams((int64_t)a.tokens * a.heads * a.dim, a.dim, DT);
     if (!wide) rotary_pairs_kernel<DT><<<grid, kThreads, 0, stream>>>(a);
     else if (il && large) rotary_kernel<DT, true, 4, DT != KVR_DT_FP32><<<grid, kThreads, 0, stream>>>(a);
@@ -213,7 +213,7 @@ hipError_t launch_rotary_table(const Freqs &f, double magnitude, int rot, int64_
 {
     const int half = rot / 2;
     const int64_t total = n_pos * half;
-    table_kernel<<<dim3((unsigned)cdiv(total, kThreads)), kThreads, 0, stream>>>(f, magnitude, half,
+    table_kernel<<<grid_of(cdiv(total, kThreads)), kThreads, 0, stream>>>(f, magnitude, half,
                                                                                total, table);
     return hipGetLastError();
 }

@@ -7,6 +7,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/core/LegacyTypeDispatch.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <hip/hip_runtime_api.h>
@@ -53,6 +54,14 @@ struct Device {
     }
 };
 
+// Calls record no gradients, so tensors that need one are refused rather than cut off.
+void no_gradient(const at::Tensor &t, const char *name)
+{
+    if (t.requires_grad() && c10::GradMode::is_enabled())
+        refuse(std::string(name) + " requires gradients, which this call does not record: detach it or "
+                                   "call under torch.no_grad()");
+}
+
 int64_t integer(PyObject *o, const char *name)
 {
     const long long x = PyLong_AsLongLong(o);
@@ -89,6 +98,7 @@ const at::Tensor &rows(PyObject *o, const char *name, Device &on, int64_t tokens
     if (!t.is_cuda() || t.dim() != 3 || (t.stride(2) != 1 && t.size(2) != 1))
         refuse(std::string(name) + " must be a [tokens, heads, dim] CUDA tensor with adjacent rows");
     on.check(t, name);
+    no_gradient(t, name);
     const int64_t want[3] = {tokens, heads, dim};
     for (int i = 0; i < 3; ++i)
         if (want[i] >= 0 && t.size(i) != want[i]) {
@@ -133,6 +143,7 @@ const at::Tensor &table_of(PyObject *o, Device &on)
         !t.is_contiguous() || t.size(2) > (1 << 20))
         refuse("table must be a contiguous [n_pos, 2, rot_dim / 2] float32 CUDA tensor");
     on.check(t, "table");
+    no_gradient(t, "table");
     return t;
 }
 int32_t rot_of(const at::Tensor &table) { return (int32_t)(2 * table.size(2)); }
@@ -147,7 +158,10 @@ const kvr_kv_cache *cache_of(PyObject *o, Device &on)
         PyErr_Clear();
         throw Refused{PyExc_TypeError, "cache must be a KvCache"};
     }
-    on.check(tensor(PyTuple_GET_ITEM(o, 1), "cache"), "cache");
+    const at::Tensor &k = tensor(PyTuple_GET_ITEM(o, 1), "cache");
+    on.check(k, "cache");
+    no_gradient(k, "cache");
+    no_gradient(tensor(PyTuple_GET_ITEM(o, 2), "cache"), "cache");
     return static_cast<const kvr_kv_cache *>(p);
 }
 

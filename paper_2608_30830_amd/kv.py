@@ -7,6 +7,8 @@ activations.  Every call enqueues on torch's current stream (or ``stream``).  Wh
 allocates (outputs and workspaces that are not given, the status of ``check``) comes from
 the current stream's memory, and ``stream`` then waits for the work queued there so far.
 Tensors and stream are of one device, which need not be the current one.
+``kvr_rotary`` is differentiable in ``x``; the other calls record no gradients and refuse
+tensors that require one (under ``torch.no_grad()`` they take them).
 With ``check`` (the default) a call waits and raises on a device-detected error;
 ``check=False`` returns without waiting, and an optional ``status`` tensor
 ([1] int32, zeroed by the caller) collects KVR_E_DOMAIN.
@@ -98,6 +100,29 @@ def load_binding():
     return module
 
 
+def _differentiable_rotary(torch):
+    """kvr_rotary as a function of x that autograd records: it is linear, and its adjoint
+    turns the gradient by the negative angles."""
+
+    class Rotary(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, positions, table, interleaved, adjoint, status, stream, check):
+            ctx.save_for_backward(positions, table)
+            ctx.way = interleaved, adjoint
+            return kvr_rotary(x, positions, table, interleaved, adjoint, None, status, stream, check)
+
+        @staticmethod
+        def backward(ctx, grad):
+            positions, table = ctx.saved_tensors
+            interleaved, adjoint = ctx.way
+            if grad.stride(2) != 1:   # an expanded one
+                grad = grad.contiguous()
+            # (positions outside the table were reported going forward)
+            return (kvr_rotary(grad, positions, table, interleaved, not adjoint, check=False),) + 7 * (None,)
+
+    return Rotary
+
+
 class _Context:
     """torch, the package, the loaded library and its binding, looked up once."""
 
@@ -107,6 +132,7 @@ class _Context:
         pkg._torch()   # raises without a GPU
         self.torch, self.pkg, self.lib = torch, pkg, pkg.load_library()
         self.fast = load_binding()
+        self.rotary = _differentiable_rotary(torch)
         self.codes = {torch.bfloat16: KVR_DT_BF16, torch.float16: KVR_DT_FP16,
                       torch.float32: KVR_DT_FP32}
 
@@ -261,6 +287,10 @@ def kvr_rotary(x, positions, table, interleaved: bool = False, adjoint: bool = F
                status=None, stream=None, check: bool = True):
     """x [tokens, heads, dim] turned by its positions; ``out`` may be ``x``."""
     c = _context()
+    if c.torch.is_grad_enabled() and getattr(x, "requires_grad", False):
+        if out is not None:
+            raise ValueError("out cannot be given where x requires gradients")
+        return c.rotary.apply(x, positions, table, interleaved, adjoint, status, stream, check)
     if check:
         status = _status(c, x, check, status, stream)
     rc, out = c.fast.rotary(x, positions, table, _flags(interleaved, adjoint), out, status,

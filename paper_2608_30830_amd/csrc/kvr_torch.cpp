@@ -212,6 +212,13 @@ struct Stream {
     }
 };
 
+// Notes for autograd that a tensor has been written: it may have been saved for a gradient.
+// (Tensors made in inference mode have no version.)
+void written(const at::Tensor &t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // A Python tuple of a status code and tensors (undefined ones: None).
 template <class... Ts>
 PyObject *answer(int rc, const Ts &...ts)
@@ -287,6 +294,8 @@ PyObject *rotary(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (!out.defined()) {
             out = new_like(x);
             stream.allocated();
+        } else {
+            written(out);
         }
         const int rc = kvr_rotary(x.data_ptr(), out.data_ptr(), dt, tokens, heads, dim, x.stride(0),
                                   x.stride(1), out.stride(0), out.stride(1), address<int32_t>(pos),
@@ -321,6 +330,8 @@ PyObject *cache_write(PyObject *, PyObject *const *a, Py_ssize_t n)
         const at::Tensor *status = status_of(a[7], on);
         const GivenStream own(a[8], on);
         const Stream stream(own, on);
+        for (int i = 1; i <= 4; ++i)   // the cache's tensors, scales among them if it has any
+            if (given(PyTuple_GET_ITEM(a[0], i))) written(tensor(PyTuple_GET_ITEM(a[0], i), "cache"));
         return answer(kvr_cache_write(c, k.data_ptr(), v.data_ptr(), dt, tokens, k.stride(0),
                                       k.stride(1), v.stride(0), v.stride(1), address<int64_t>(slots),
                                       address<int32_t>(pos), address<float>(t), t ? t->size(0) : 0,
@@ -361,6 +372,9 @@ PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n)
             k = at::empty({tokens, heads, dim}, options);
             v = at::empty({tokens, heads, dim}, options);
             stream.allocated();
+        } else {
+            written(k);
+            written(v);
         }
         const int rc = kvr_cache_read(c, address<int64_t>(slots), tokens, k.data_ptr(), v.data_ptr(),
                                       dt, k.stride(0), k.stride(1), v.stride(0), v.stride(1),
@@ -429,6 +443,8 @@ PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (!out.defined()) {
             out = new_like(q);
             allocated = true;
+        } else {
+            written(out);
         }
         if (want_lse) {
             lse = at::empty({q.size(0), q.size(1)}, q.options().dtype(at::kFloat));

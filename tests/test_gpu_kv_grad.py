@@ -107,3 +107,40 @@ def test_lost_gradients_are_refused(kvr):
             call(leaf)
         with torch.inference_mode():
             call(leaf)
+
+
+def test_written_tensors_are_noticed(kvr):
+    """A tensor that autograd has saved and a call then writes: backward says so, as after
+    torch's own operations in place."""
+    import torch
+    cache = kvr.KvCache.allocate(kvr.KVR_KV_BF16, 4, 2, 16, 64)
+    x = _randn(1, (5, 2, 64), "bf16")
+    slots, pos = torch.arange(5, device="cuda"), torch.arange(5, device="cuda").int()
+    table = _table(2, 8, 64)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    att = (torch.tensor([0, 2], **i32), torch.tensor([5], **i32), torch.zeros(1, 1, **i32), 2, 5)
+    q, out = _randn(3, (2, 4, 64), "bf16"), torch.empty(2, 4, 64, dtype=torch.bfloat16, device="cuda")
+    a, b, y = (torch.empty_like(x) for _ in range(3))
+    writes = [(cache.k, lambda: kvr.kvr_cache_write(cache, x, x, slots)),
+              (cache.v, lambda: kvr.kvr_cache_write(cache, x, x, slots, check=False)),
+              (a, lambda: kvr.kvr_cache_read(cache, slots, out=(a, b))),
+              (b, lambda: kvr.kvr_cache_read(cache, slots, out=(a, b))),
+              (y, lambda: kvr.kvr_rotary(x, pos, table, out=y)),
+              (out, lambda: kvr.kvr_tree_attention(cache, q, *att, out=out))]
+    for t, write in writes:
+        w = torch.ones_like(t, requires_grad=True)
+        loss = (w * t).sum()          # saves t
+        kvr.kvr_cache_read(cache, slots)
+        kvr.kvr_tree_attention(cache, q, *att)
+        loss.backward(retain_graph=True)
+        write()
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    quant = kvr.KvCache.allocate(kvr.KVR_KV_FP4, 4, 2, 16, 64)
+    before = [t._version for t in quant.tensors]
+    kvr.kvr_cache_write(quant, x, x, slots)
+    assert [t._version for t in quant.tensors] == [n + 1 for n in before]
+    with torch.inference_mode():
+        kvr.kvr_cache_write(quant, x, x, slots)
+        own = torch.empty_like(x)
+    kvr.kvr_rotary(x, pos, table, out=own)      # has no version

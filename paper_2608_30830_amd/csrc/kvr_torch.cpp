@@ -426,7 +426,11 @@ PyObject *tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
                 throw Refused{PyExc_TypeError, "scale must be a number"};
             }
         }
-        const bool want_lse = PyObject_IsTrue(a[9]);
+        const int want_lse = PyObject_IsTrue(a[9]);
+        if (want_lse < 0) {
+            PyErr_Clear();
+            throw Refused{PyExc_TypeError, "want_lse must be true or false"};
+        }
         at::Tensor out = given_like(a[10], q, on, "out must have the type of q");
         at::Tensor lse, ws;
         if (given(a[11])) {

@@ -95,3 +95,13 @@ def test_attention(fast, on):
     for bad in ("q", "cu_q", "kv_len", "page_table", "tree_mask", "out", "workspace", "status", "stream"):
         with pytest.raises(ValueError, match=f"{bad} must be o.* cuda:0"):
             call(bad)
+
+
+def test_want_lse_without_a_truth_value(fast, on):
+    class Neither:
+        def __bool__(self):
+            raise RuntimeError("no")
+
+    with pytest.raises(TypeError, match="want_lse"):
+        fast.tree_attention(_cache(on).handle, on(0, (6, 4, 64)), on(0, (3,), torch.int32), on(0, (2,), torch.int32),
+                            on(0, (2, 3), torch.int32), 3, 40, None, None, Neither(), None, None, None, None)

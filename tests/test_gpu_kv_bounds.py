@@ -23,8 +23,9 @@ def _workspace_bytes(kvr, p, n_seqs):
                           pages_stride=p.table.shape[1], max_pages=p.table.shape[1], n_queries=p.q.shape[0],
                           n_seqs=n_seqs, max_q=p.max_q, max_kv=p.max_kv)
     n = ctypes.c_size_t(0)
+    dtype = kvr.KVR_DT_BF16 if p.dtype == "bf16" else kvr.KVR_DT_FP16
     rc = kvr.load_library().kvr_tree_attention(
-        ctypes.byref(p.cache.c), ctypes.byref(s), None, kvr.KVR_DT_BF16, p.q.shape[1], 0, 0, None, 0, 1.0, None, 0, 0,
+        ctypes.byref(p.cache.c), ctypes.byref(s), None, dtype, p.q.shape[1], 0, 0, None, 0, 1.0, None, 0, 0,
         None, None, None, ctypes.byref(n), None)
     assert rc == kvr.KVR_OK
     return n.value

@@ -1085,12 +1085,10 @@ template <int FMT, int QT>
 hipError_t launch_dim(const Attention &a, dim3 grid, hipStream_t stream)
 {
     switch (a.c.dim) {
-#ifndef KVR_DEV_DIM128
     case 64: return launch_nb<FMT, QT, 2>(a, grid, stream);
     case 96: return launch_nb<FMT, QT, 3>(a, grid, stream);
     case 192: return launch_nb<FMT, QT, 6>(a, grid, stream);
     case 256: return launch_nb<FMT, QT, 8>(a, grid, stream);
-#endif
     default: return launch_nb<FMT, QT, 4>(a, grid, stream);
     }
 }

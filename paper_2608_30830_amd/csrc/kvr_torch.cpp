@@ -187,12 +187,13 @@ struct GivenStream {
 // current device as long as this lives: a launch goes to the current device, whatever
 // device its tensors are on.  Made when every argument has been checked.
 struct Stream {
-    c10::hip::HIPGuard device;
+    c10::hip::OptionalHIPGuard device;
     hipStream_t current, used;
     Stream(const GivenStream &s, const Device &on)
-        : device(on.at.index()), current(c10::hip::getCurrentHIPStream(on.at.index()).stream()),
+        : current(c10::hip::getCurrentHIPStream(on.at.index()).stream()),
           used(s.any ? s.handle : current)
     {
+        if (c10::hip::current_device() != on.at.index()) device.set_index(on.at.index());
     }
     // After an allocation: memory comes from the current stream's pool, where work on what it
     // held before may still be queued, and another stream waits for that.

@@ -287,7 +287,7 @@ def kvr_rotary(x, positions, table, interleaved: bool = False, adjoint: bool = F
                status=None, stream=None, check: bool = True):
     """x [tokens, heads, dim] turned by its positions; ``out`` may be ``x``."""
     c = _context()
-    if c.torch.is_grad_enabled() and getattr(x, "requires_grad", False):
+    if getattr(x, "requires_grad", False) and c.torch.is_grad_enabled():
         if out is not None:
             raise ValueError("out cannot be given where x requires gradients")
         return c.rotary.apply(x, positions, table, interleaved, adjoint, status, stream, check)

@@ -19,13 +19,14 @@
 // With up to 32 rows every wave has all of them and takes every n-th step of 32
 // tokens, with the loads of the next steps in flight and their pages looked up a
 // round earlier; a block joins its waves through LDS.  Memory bounds this: 64
-// sequences of 8,192 tokens, 8 heads of 128, one new token each: 188 us in 8
-// bits (5.9 TB/s of cache), 374 us in 16 (5.7), 120 us in 4 (4.8, where the
+// sequences of 8,192 tokens, 8 heads of 128, one new token each: 190 us in 8
+// bits (5.8 TB/s of cache), 373 us in 16 (5.8), 117 us in 4 (4.9, where the
 // conversions begin to count).  With more rows the waves divide them and share
 // the tokens through LDS, converted and turned around once: 16 sequences of
-// 16,384 tokens and 512 rows, 16 bits: 0.66 ms, 830 TFLOP/s.  There the matrix
-// unit is busy for 39 % of the cycles and the vector unit for 43 % (the softmax: a
-// multiply-add, an exponential, a sum and a maximum a score), and with the two
+// 16,384 tokens and 512 rows, 16 bits: 0.67 ms, 820 TFLOP/s.  There the matrix
+// unit is busy for 40 % of the cycles and the vector unit for 44 % (the softmax: a
+// multiply-add, an exponential, a sum and half a packing a score, and 20 instructions for
+// the maximum of 16, half of which only quiet NaNs), and with the two
 // waves that the registers leave a SIMD their sum is what counts: reading LDS
 // further ahead, a second buffer in place of one of the two barriers and the
 // weights of one step interleaved with the products of the other by hand changed
@@ -603,7 +604,11 @@ struct Kernel {
         }
     }
 
-    // The weights of a row tile's scores, in the products' type.
+    // The weights of a row tile's scores, in the products' type: 16 bits, which the matrix
+    // instructions take; 32 would be two products in place of one.  Scores, sums and outputs stay in
+    // 32.  The outputs' error against 64 bits, most of it their own rounding to bfloat16, is
+    // 0.0019 of them with it and 0.0017 without for one token over 1,000, 0.0018 and 0.0017 over
+    // 8,192 in 8 bits, 0.0022 and 0.0017 for trees over 2,048 to 32,768 tokens.
     template <int R>
     __device__ __forceinline__ void weights(const f32x4 (&sc)[2], State &st, u32x4 (&pv)[QS]) const
     {

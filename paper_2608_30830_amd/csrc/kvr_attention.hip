@@ -126,8 +126,8 @@ hipError_t launch_combine(const Attention &a, hipStream_t stream)
     const int64_t rows = (int64_t)a.max_q * a.group;
     const bool many = rows * a.c.n_heads * a.n_seqs >= 4096;
     const bool narrow = a.c.dim <= 128;
-    // Many parts of few sequences: a block of 1,024 (one sequence of 90,196 tokens and one KV
-    // head, 470 parts: 27 -> 21 us a call; with 96 parts of 56 rows 73 -> 75).
+    // Many parts of few sequences: a block of 1,024 (one sequence of 90,196 tokens in 4 bits and
+    // one KV head, 470 parts: 24.5 -> 18.7 us a call; with 96 parts of 56 rows 73 -> 75).
     const int64_t parts = std::min<int64_t>(a.target / a.n_seqs, cdiv(a.max_kv, kStep) / a.min_steps);
     const bool deep = !many && parts > 128;
     const int threads = deep ? 1024 : 256;
@@ -144,8 +144,9 @@ hipError_t launch_combine(const Attention &a, hipStream_t stream)
 // Blocks that the parts are planned for, of all heads: what is resident at once (two
 // blocks on each of 256 CUs, three where 64 rows share tokens), so that equal parts
 // end together; twice that where each block has 128 rows, because there the rows of
-// ragged sequences fill blocks unevenly (tree of up to 64 tokens over 2,048 to 32,768:
-// 501 us planned for 512, 417 for 1,024, 423 for 2,048 and more joining).
+// ragged sequences fill blocks unevenly (trees of 17 to 64 tokens over 2,048 to 32,768:
+// 364 us planned for 512, 350 for 1,024, 344 for 2,048; 512 rows of each sequence over
+// 16,384 tokens: 650, 671, 695).
 constexpr int kSlots = 512;
 constexpr int kShortSteps = 16;    // 512 tokens
 
@@ -165,17 +166,17 @@ size_t plan_attention(Attention &a)
     a.row_tiles = rows <= 16 || !narrow || (rows > 32 && rows <= 64) ? 1 : 2;
     a.waves = 4;
     // A part's outputs (32 bits) are written and read again: of 128 rows they are worth 8 steps
-    // of 16-bit cache (24 sequences of 63 to 184 tokens, 63 new ones, 8 queries a head: 56 us in
-    // parts of four steps, 35 in parts of 16).
+    // of 16-bit cache (24 sequences of 63 to 184 tokens, 63 new ones, 8 queries a head: 50 us in
+    // parts of four steps, 31 in parts of 16).
     a.min_steps = a.shared ? 8 * a.row_tiles : a.waves;
     int slots = kSlots;
     if (a.shared) slots = a.row_tiles > 1 ? 2 * kSlots : kSlots * 3 / 2;
     // Short sequences: no parts, so that one launch does, and eight waves a block while the
     // blocks are not more than the CUs.  (Bfloat16, 8 heads of 128, us a call against parts: one
-    // sequence of 500 tokens 10.5, 11.1; of 1,000 14.7, 11.2; 32 of 500 15.8, 20.6; of 1,000
-    // 24.0, 28.3; 128 of 2,000 180, 184; 400 of 50 to 2,000 171, 203: where sequences are many,
+    // sequence of 500 tokens 10.6, 12.0; of 1,000 14.7, 11.8; 32 of 500 16.0, 20.9; of 1,000
+    // 24.1, 28.7; 128 of 2,000 179, 184; 400 of 50 to 2,000 171, 203: where sequences are many,
     // finding the parts and joining them is not free.  With 24 rows a head in 8 bits: one of 500 tokens
-    // 11.0, 12.8; 32 of 500 13.1, 18.8; 200 of 500 51, 77; 200 of 2,000 170, 195.)
+    // 11.3, 12.8; 32 of 500 13.6, 19.0; 200 of 500 54, 81; 200 of 2,000 180, 208.)
     const int64_t heads = (int64_t)a.n_seqs * a.c.n_heads;
     if (!a.shared && longest <= kShortSteps * (heads >= 1024 ? 4 : heads >= 128 ? 2 : 1)) {
         a.waves = rows <= 16 && heads <= 256 ? 8 : 4;

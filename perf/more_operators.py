@@ -1,0 +1,678 @@
+"""The latent cache and the life of a cache's pages, and what is measured of them.
+
+A latent cache keeps one vector a token for all heads: `rank` elements that stand for every head's key
+and value, and `rot` elements of a key that all heads share and that carries the position.  Four
+operators, each over the range that serving suspended agents meets:
+
+``write``      kvr_latent_write: latents (normalised) and shared keys (rotated) of new tokens into the
+               pages, in 16 bits or quantised to 8, then kvr_latent_read of the same rows
+``attention``  kvr_latent_attention: one new token, a run, or a tree of drafted tokens of each sequence
+               over its pages, queries and outputs in the latent's space (the absorbed form)
+``prompt``     kvr_latent_prompt: prompts, or their next chunks, with keys and values expanded for each
+               head and the one rotated part that the heads share
+``pages``      kvr_pages_fork, kvr_pages_resize, kvr_pages_copy and kvr_pages_compact: agents that
+               branch, grow and end over one pool of pages, and the pool brought together
+
+A row in 8 bits is cut into blocks of 32; a block keeps one power of two (a byte: its exponent + 127) and
+32 codes (e4m3).
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+DTYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+LARGEST = 448.0     # the largest code
+MIN_EXP = -110      # the smallest block exponent
+EPS = 1e-6          # of the latent's norm
+
+
+def listed():
+    return [
+        # one decoded token of one agent: the smallest call, latency only
+        dict(name="write-1-token", op="write", fmt="bf16", tokens=1, rank=512, rot=64, dtype="bf16",
+             norm=True, interleaved=True, page=16, positions=131072, skip=0),
+        # a context recomputed and kept in 8 bits, odd length, some rows padding
+        dict(name="write-32k-fp8", op="write", fmt="fp8", tokens=32749, rank=512, rot=64, dtype="bf16",
+             norm=True, interleaved=False, page=64, positions=32768, skip=100),
+        # one resumed agent, one token over a short context: latency
+        dict(name="attention-1x1000", op="attention", fmt="bf16", dtype="bf16", seqs=1, kv_lo=1000,
+             kv_hi=1000, q_lo=1, q_hi=1, tree=False, heads=16, rank=512, rot=64, page=16, shape_seed=1),
+        # the decode step of 64 agents of 8,192 tokens each, 16 heads a GPU, in 8 bits
+        dict(name="attention-64x8192-fp8", op="attention", fmt="fp8", dtype="bf16", seqs=64, kv_lo=8192,
+             kv_hi=8192, q_lo=1, q_hi=1, tree=False, heads=16, rank=512, rot=64, page=64, shape_seed=2),
+        # sixteen agents of 2,048 to 32,768 tokens, all 128 heads on one GPU
+        dict(name="attention-16-ragged-h128", op="attention", fmt="bf16", dtype="bf16", seqs=16,
+             kv_lo=2048, kv_hi=32768, q_lo=1, q_hi=1, tree=False, heads=128, rank=512, rot=64, page=32,
+             shape_seed=3),
+        # one agent of the longest context, a small tree of drafted tokens, a narrower latent
+        dict(name="attention-1x128k-tree9", op="attention", fmt="fp16", dtype="fp16", seqs=1,
+             kv_lo=131071, kv_hi=131071, q_lo=9, q_hi=9, tree=True, heads=16, rank=256, rot=64, page=64,
+             shape_seed=4),
+        # a few short prompts of odd lengths, small heads: latency
+        dict(name="prompt-5-short", op="prompt", dtype="fp16", seqs=5, q_lo=17, q_hi=500, past=0, heads=8,
+             group=1, nope=64, rot=32, causal=True, shape_seed=5),
+        # one context of 8,192 tokens recomputed after its copy was discarded
+        dict(name="prompt-1x8192", op="prompt", dtype="bf16", seqs=1, q_lo=8192, q_hi=8192, past=0,
+             heads=32, group=1, nope=128, rot=64, causal=True, shape_seed=6),
+        # the next 509 tokens of two agents of 16,384 restored ones
+        dict(name="prompt-2x509-after-16k", op="prompt", dtype="bf16", seqs=2, q_lo=509, q_hi=509,
+             past=16384, heads=20, group=1, nope=128, rot=64, causal=True, shape_seed=7),
+        # one agent branches once: latency of the bookkeeping
+        dict(name="pages-1-branch", op="pages", kind="branch", parents=1, branches=1, len_lo=1000,
+             len_hi=1000, grow=8, page=16, spare=64, cache="latent", layers=2, heads=1, dim=512, rot=64,
+             dtype="bf16", shape_seed=8),
+        # 32 agents try four continuations each
+        dict(name="pages-32x4-branches", op="pages", kind="branch", parents=32, branches=4, len_lo=1024,
+             len_hi=8192, grow=150, page=64, spare=700, cache="kv", layers=2, heads=8, dim=128, rot=0,
+             dtype="bf16", shape_seed=9),
+        # a pool that ended agents left full of holes is brought together
+        dict(name="pages-compact-4k", op="pages", kind="compact", parents=48, branches=1, len_lo=500,
+             len_hi=8192, grow=0, page=64, spare=2048, cache="latent", layers=6, heads=1, dim=512, rot=64,
+             dtype="fp16", shape_seed=10),
+    ]
+
+
+def log_int(rng, lo, hi):
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    op = rng.choice(["write", "attention", "attention", "prompt", "prompt", "pages"])
+    seed = rng.randint(0, 10 ** 6)
+    rank, rot = rng.choice([256, 512, 512]), rng.choice([32, 64, 64])
+    if op == "write":
+        fmt = rng.choice(["bf16", "fp16", "fp8", "fp8"])
+        dtype = fmt if fmt in DTYPES else rng.choice(["bf16", "fp32"])
+        tokens = log_int(rng, 1, 32749 if dtype != "fp32" else 16384)
+        return dict(op=op, fmt=fmt, tokens=tokens, rank=rank, rot=rot, dtype=dtype, norm=rng.random() < 0.7,
+                    interleaved=rng.random() < 0.5, page=rng.choice([16, 32, 64, 256]), positions=32768,
+                    skip=tokens // 50 if rng.random() < 0.5 else 0)
+    if op == "attention":
+        fmt = rng.choice(["bf16", "fp16", "fp8", "fp8"])
+        heads, seqs = rng.choice([1, 8, 16, 16, 20, 64, 128]), log_int(rng, 1, 64)
+        q_hi = rng.choice([1, 1, log_int(rng, 2, 24)])
+        # no dearer than the listed ones: cache elements, and products of rows and elements
+        tokens = min(64 * 8192, 16 * 11000 * 128 // (q_hi * heads))
+        kv_hi = log_int(rng, q_hi, max(q_hi, min(131072, tokens // seqs)))
+        return dict(op=op, fmt=fmt, dtype=fmt if fmt in DTYPES else "bf16", seqs=seqs,
+                    kv_lo=max(q_hi, kv_hi // rng.choice([1, 4, 16])), kv_hi=kv_hi,
+                    q_lo=rng.choice([q_hi, max(1, q_hi // 3)]), q_hi=q_hi,
+                    tree=q_hi > 1 and rng.random() < 0.7, heads=heads, rank=rank, rot=rot,
+                    page=rng.choice([16, 32, 64, 256]), shape_seed=seed)
+    if op == "prompt":
+        heads, group = rng.choice([1, 5, 8, 20, 32, 32]), rng.choice([1, 1, 1, 2])
+        q_hi, seqs = log_int(rng, 1, 8192), rng.randint(1, 8)
+        pairs = 8192 * 8192 // 2 * 32 // (heads * group * seqs)
+        q_hi = min(q_hi, int(math.sqrt(pairs)))
+        past = min(32768, rng.choice([0, 0, log_int(rng, 1, 32768)]), pairs // q_hi - q_hi)
+        return dict(op=op, dtype=rng.choice(["bf16", "bf16", "fp16"]), seqs=seqs,
+                    q_lo=max(1, q_hi // rng.choice([1, 4, 16])), q_hi=q_hi, past=max(0, past), heads=heads,
+                    group=group, nope=rng.choice([64, 128, 128]), rot=rot, causal=rng.random() < 0.8,
+                    shape_seed=seed)
+    kv = rng.random() < 0.5
+    hi = log_int(rng, 100, 8192)
+    parents = log_int(rng, 1, min(64, 200000 // hi))
+    return dict(op=op, kind=rng.choice(["branch", "compact"]), parents=parents, branches=rng.randint(1, 4),
+                len_lo=max(1, hi // rng.choice([1, 5])), len_hi=hi, grow=rng.randint(1, 150),
+                page=rng.choice([16, 64, 64, 256]), spare=rng.randint(300, 1000),
+                cache="kv" if kv else "latent", layers=rng.randint(1, 2 if kv else 4),
+                heads=rng.choice([1, 4, 8]) if kv else 1, dim=128 if kv else rank, rot=0 if kv else rot,
+                dtype=rng.choice(["bf16", "fp16"]), shape_seed=seed)
+
+
+def lengths(case):
+    """Each sequence's tokens in the cache, its newest ones among them, and how many those are."""
+    rng = random.Random(case["shape_seed"])
+    if case["op"] == "prompt":
+        nq = [log_int(rng, case["q_lo"], case["q_hi"]) for _ in range(case["seqs"])]
+        return [n + case["past"] for n in nq], nq
+    if case["op"] == "pages":
+        return [log_int(rng, case["len_lo"], case["len_hi"]) for _ in range(case["parents"])], None
+    kv = [log_int(rng, case["kv_lo"], case["kv_hi"]) for _ in range(case["seqs"])]
+    return kv, [min(n, rng.randint(case["q_lo"], case["q_hi"])) for n in kv]
+
+
+def row_bytes(case):
+    """A row of the latent cache."""
+    dim = case["rank"] + case["rot"]
+    return dim + dim // 32 if case["fmt"] == "fp8" else 2 * dim
+
+
+def work(case):
+    c = case
+    size = {"bf16": 2, "fp16": 2, "fp32": 4}[c["dtype"]]
+    if c["op"] == "write":
+        dim = c["rank"] + c["rot"]
+        # in and into the cache, back and out
+        return {"bytes": c["tokens"] * (2 * dim * size + 2 * row_bytes(c) + 4 * c["rot"] + 20),
+                "flops": c["tokens"] * (4 * c["rank"] + 6 * c["rot"])}
+    if c["op"] == "pages":
+        lens, _ = lengths(c)
+        page = c["page"]
+        one = 2 * c["page"] * (c["dim"] + c["rot"]) * c["heads"] * c["layers"] * (2 if c["cache"] == "kv" else 1)
+        held = sum(-(-n // page) for n in lens)
+        if c["kind"] == "branch":
+            shared = sum(n % page != 0 for n in lens) * c["branches"]
+            entries = c["branches"] * sum(2 * -(-n // page) + -(-(n + c["grow"]) // page) for n in lens)
+            return {"bytes": 2 * one * shared + 4 * (held + c["spare"]) + 8 * entries, "flops": 0}
+        total = 2 * held + c["spare"]
+        # of the pages in use, spread evenly, those beyond as many as are in use
+        return {"bytes": 2 * one * held * (total - held) // total + 8 * total + 8 * held, "flops": 0}
+    kv, nq = lengths(c)
+    if c["op"] == "prompt":
+        heads = c["heads"] * c["group"]
+        dim = c["nope"] + c["rot"]
+        pairs = sum(n * t - (n * (n - 1) // 2 if c["causal"] else 0) for t, n in zip(kv, nq))
+        return {"bytes": size * (sum(nq) * heads * (dim + c["nope"])
+                                 + sum(kv) * (2 * c["heads"] * c["nope"] + c["rot"])) + 4 * sum(nq) * heads,
+                "flops": 2 * pairs * heads * (dim + c["nope"])}
+    dim = c["rank"] + c["rot"]
+    return {"bytes": sum(kv) * row_bytes(c) + sum(nq) * c["heads"] * (size * (dim + c["rank"]) + 4),
+            "flops": sum(2 * n * c["heads"] * (dim + c["rank"]) * (t - (n - 1) / 2) for t, n in zip(kv, nq))}
+
+
+# ---- inputs -------------------------------------------------------------------------------------
+
+def rotary_table(positions, rot):
+    """cos and sin of position * 10000^(-2i / rot), [positions, 2, rot / 2]."""
+    freq = 10000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64, device="cuda") / rot)
+    angle = torch.arange(positions, dtype=torch.float64, device="cuda")[:, None] * freq
+    return torch.stack([angle.cos(), angle.sin()], 1).float()
+
+
+def activations(gen, shape, dtype):
+    """Projections of a hidden state: near normal, some channels several times larger."""
+    x = torch.randn(shape, generator=gen, device="cuda", dtype=torch.float32)
+    wide = 1 + 4 * (torch.rand(shape[-1], generator=gen, device="cuda") < 0.05)
+    return (x * wide).to(dtype)
+
+
+def filled_rows(gen, case, pages):
+    """The latent cache's tensors, every row written: [pages, page, row]."""
+    dim = case["rank"] + case["rot"]
+    shape = (pages, case["page"], dim)
+    if case["fmt"] in DTYPES:
+        return dict(rows=activations(gen, shape, DTYPES[case["fmt"]]), scale=None)
+    codes, scale = encode(activations(gen, shape, torch.bfloat16))
+    return dict(rows=codes, scale=scale)
+
+
+def empty_rows(case, pages):
+    dim, shape = case["rank"] + case["rot"], (pages, case["page"])
+    if case["fmt"] in DTYPES:
+        return dict(rows=torch.zeros(shape + (dim,), dtype=DTYPES[case["fmt"]], device="cuda"), scale=None)
+    return dict(rows=torch.zeros(shape + (dim,), dtype=torch.uint8, device="cuda"),
+                scale=torch.zeros(shape + (dim // 32,), dtype=torch.uint8, device="cuda"))
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def starts(n):
+    out = [0]
+    for x in n:
+        out.append(out[-1] + x)
+    return ints(out)
+
+
+def prepare(case, seed):
+    gen = torch.Generator("cuda").manual_seed(seed)
+    c = dict(case)
+    s = {"case": c}
+    if c["op"] == "write":
+        prepare_write(s, c, gen)
+    elif c["op"] == "attention":
+        prepare_attention(s, c, gen, seed)
+    elif c["op"] == "prompt":
+        prepare_prompt(s, c, gen)
+    else:
+        prepare_pages(s, c, gen)
+    if own:
+        import paper_2608_30830_amd as kvr
+        if c["op"] in ("write", "attention"):   # the framework's handles, which a program makes once
+            s["handle"] = kvr.LatentCache(s["cache"]["rows"], c["rot"], s["cache"]["scale"])
+        elif c["op"] == "pages":
+            s["buffers"] = kvr.PageBuffers([kvr.KvCache(*x) if c["cache"] == "kv"
+                                            else kvr.LatentCache(x[0], c["rot"]) for x in s["caches"]])
+    return s
+
+
+def prepare_write(s, c, gen):
+    s["table"] = rotary_table(c["positions"], c["rot"])
+    # a decoded token's position is anywhere, a context's tokens follow one another
+    first = torch.randint(0, max(1, c["positions"] - c["tokens"]), (1,), generator=gen, device="cuda")
+    s["positions"] = ((first + torch.arange(c["tokens"], device="cuda")) % c["positions"]).int()
+    # one projection gives both parts
+    x = activations(gen, (c["tokens"], c["rank"] + c["rot"]), DTYPES[c["dtype"]])
+    s["latent"], s["key"] = x[:, :c["rank"]], x[:, c["rank"]:]
+    s["weight"] = None
+    if c["norm"]:
+        s["weight"] = (1 + 0.2 * torch.randn(c["rank"], generator=gen, device="cuda")).to(DTYPES[c["dtype"]])
+    used = -(-c["tokens"] // c["page"])
+    pages = used + 1 + used // 8
+    order = torch.randperm(pages, generator=gen, device="cuda")[:used]
+    slots = (order[:, None] * c["page"] + torch.arange(c["page"], device="cuda")).reshape(-1)
+    s["slots"] = slots[:c["tokens"]].clone()
+    if c["skip"]:   # padding of the batch: written nowhere
+        s["slots"][torch.randperm(c["tokens"], generator=gen, device="cuda")[:c["skip"]]] = -1
+    s["cache"] = empty_rows(c, pages)
+
+
+def prepare_attention(s, c, gen, seed):
+    kv, nq = lengths(c)
+    need = [-(-n // c["page"]) for n in kv]
+    pages = sum(need) + 1
+    s["page_table"] = page_rows(need, torch.randperm(pages, generator=gen, device="cuda").int(), max(need))
+    s["kv_len"], s["cu_q"] = ints(kv), starts(nq)
+    s["max_q"], s["max_kv"] = max(nq), max(kv)
+    dim = c["rank"] + c["rot"]
+    # an absorbed query sums over the channels of a head: wider than one of its own
+    s["q"] = activations(gen, (sum(nq), c["heads"], dim), DTYPES[c["dtype"]])
+    s["scale"] = (128 + c["rot"]) ** -0.5 * (192.0 / dim) ** 0.5
+    s["mask"] = None
+    if c["tree"]:
+        rng, words = random.Random(seed), []
+        for n in nq:
+            seen = []
+            for i in range(n):   # a drafted token sees itself and what its parent sees
+                parent = rng.randint(max(-1, i - 8), i - 1)
+                seen.append((seen[parent] if parent >= 0 else 0) | 1 << i)
+            words += seen
+        s["mask"] = torch.tensor(words, dtype=torch.int64, device="cuda")[:, None]
+    s["cache"] = filled_rows(gen, c, pages)
+
+
+def page_rows(need, order, width):
+    """Page tables of sequences that hold so many pages each, taken from `order`."""
+    table = torch.full((len(need), width), -1, dtype=torch.int32, device="cuda")
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    return table
+
+
+def prepare_prompt(s, c, gen):
+    kv, nq = lengths(c)
+    dtype = DTYPES[c["dtype"]]
+    s["cu_q"], s["cu_k"], s["max_q"], s["max_k"] = starts(nq), starts(kv), max(nq), max(kv)
+    s["q"] = activations(gen, (sum(nq), c["heads"] * c["group"], c["nope"] + c["rot"]), dtype)
+    # one product of the latents gives both
+    x = activations(gen, (sum(kv), c["heads"], 2 * c["nope"]), dtype)
+    s["k"], s["v"] = x[..., :c["nope"]], x[..., c["nope"]:]
+    s["k_rot"] = activations(gen, (sum(kv), c["rot"]), dtype)
+
+
+def prepare_pages(s, c, gen):
+    lens, _ = lengths(c)
+    page, branches = c["page"], c["branches"]
+    held = [-(-n // page) for n in lens]
+    if c["kind"] == "branch":   # rows of the agents, then of what they branch into
+        rows = len(lens) * (1 + branches)
+        n_pages, width = sum(held) + c["spare"], -(-(max(lens) + c["grow"]) // page) + 1
+        n_pages += branches * sum(-(-(n + c["grow"]) // page) - n // page for n in lens)
+        s["kv_len"] = ints(lens + [0] * (rows - len(lens)))
+        s["parent"] = ints([-1] * len(lens) + [i for i in range(len(lens)) for _ in range(branches)])
+        s["ended"] = ints([-1] * len(lens) + [0] * (rows - len(lens)))
+        s["grown"] = ints([-1] * len(lens) + [n + c["grow"] for n in lens for _ in range(branches)])
+        need = held + [0] * (rows - len(lens))
+    else:
+        n_pages, width, need = 2 * sum(held) + c["spare"], max(held), held
+        s["kv_len"] = ints(lens)
+    order = torch.randperm(n_pages, generator=gen, device="cuda").int()[:sum(held)]
+    s["page_table"] = page_rows(need, order, width)
+    s["refs"] = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+    s["refs"][order.long()] = 1
+    dim = c["dim"] + c["rot"]
+    shape = (n_pages, c["heads"], page, dim) if c["cache"] == "kv" else (n_pages, page, dim)
+    each = 2 if c["cache"] == "kv" else 1
+    s["caches"] = [[activations(gen, shape, DTYPES[c["dtype"]]) for _ in range(each)] for _ in range(c["layers"])]
+
+
+# ---- the plain forms ----------------------------------------------------------------------------
+
+def rotate(x, positions, table, interleaved):
+    """Rotary positions of rows [tokens, rot] in 32 bits."""
+    rows = table[positions.long()]
+    cos, sin = rows[:, 0], rows[:, 1]
+    a, b = (x[..., 0::2], x[..., 1::2]) if interleaved else x.chunk(2, -1)
+    y, z = a * cos - b * sin, b * cos + a * sin
+    return torch.stack([y, z], -1).flatten(-2) if interleaved else torch.cat([y, z], -1)
+
+
+def encode(x):
+    """Codes and scale bytes of rows [..., dim]."""
+    blocks = x.float().unflatten(-1, (-1, 32))
+    bits = blocks.abs().amax(-1).view(torch.int32)
+    # the smallest k with amax <= 448 2^k: one more than the floor where the mantissa is beyond 1.75
+    k = (((bits + 0x7FFFFF - 0x600000) >> 23) - 127 - 8).clamp(min=MIN_EXP)
+    y = blocks * ((127 - k) << 23).view(torch.float32)[..., None]
+    return y.flatten(-2).to(torch.float8_e4m3fn).view(torch.uint8), (k + 127).to(torch.uint8)
+
+
+def decode(rows, scale):
+    """The values of rows of the cache in 32 bits."""
+    if scale is None:
+        return rows.float()
+    s = (scale.int() << 23).view(torch.float32)
+    return (rows.view(torch.float8_e4m3fn).float().unflatten(-1, (-1, 32)) * s[..., None]).flatten(-2)
+
+
+def write(s):
+    c, cache, slots = s["case"], s["cache"], s["slots"]
+    x = s["latent"].float()
+    if s["weight"] is not None:
+        x = x * torch.rsqrt(x.square().mean(-1, keepdim=True) + EPS) * s["weight"].float()
+    x = torch.cat([x, rotate(s["key"].float(), s["positions"], s["table"], c["interleaved"])], -1)
+    page = c["page"]
+    keep = slots >= 0
+    at, off = slots[keep] // page, slots[keep] % page
+    if cache["scale"] is None:
+        cache["rows"][at, off] = x[keep].to(cache["rows"].dtype)
+    else:
+        cache["rows"][at, off], cache["scale"][at, off] = encode(x[keep])
+    at, off = slots.clamp(min=0) // page, slots.clamp(min=0) % page
+    y = decode(cache["rows"][at, off], None if cache["scale"] is None else cache["scale"][at, off])
+    return torch.where((slots >= 0)[:, None], y, 0.0).to(DTYPES[c["dtype"]])
+
+
+def softmax_products(score, seen, v):
+    """Rows of softmax(score) v and the logarithms of the sums; rows that see nothing: zeros, -infinity.
+    score [..., rows, tokens], which is overwritten, v [..., tokens, dim]."""
+    score = score.masked_fill_(~seen, -math.inf)
+    top = score.amax(-1, keepdim=True)
+    top = torch.where(top == -math.inf, 0.0, top)
+    p = score.sub_(top).exp_()
+    total = p.sum(-1, keepdim=True)
+    out = torch.matmul(p, v) / torch.where(total > 0, total, 1.0)
+    return out, (top + torch.log(total))[..., 0]
+
+
+def attend(s):
+    c, cache, q, cu, kv_len = s["case"], s["cache"], s["q"], s["cu_q"].long(), s["kv_len"].long()
+    total, mq, length, heads = q.shape[0], s["max_q"], s["max_kv"], q.shape[1]
+    table = s["page_table"].clamp(min=0).long()
+    rows = decode(cache["rows"][table], None if cache["scale"] is None else cache["scale"][table])
+    rows = rows.flatten(1, 2)[:, :length]                                # [seqs, length, dim]
+    t = torch.arange(length, device=q.device)
+    rows = torch.where((t < kv_len[:, None])[..., None], rows, 0.0)
+    nq = cu[1:] - cu[:-1]
+    i = torch.arange(mq, device=q.device)
+    at = (cu[:-1, None] + i).clamp(max=total - 1)
+    x = q.float()[at].flatten(1, 2)                                      # [seqs, mq * heads, dim]
+    score = torch.matmul(x, rows.transpose(1, 2)).mul_(s["scale"])
+    newest = t - (kv_len - nq)[:, None]                                  # from 0 for drafted ones
+    if s["mask"] is None:
+        seen = newest[:, None] <= i[:, None]
+    else:
+        bits = ((s["mask"][at][..., 0][..., None] >> i) & 1).bool()      # [seqs, mq, mq]
+        m = newest.clamp(0, mq - 1)[:, None].expand(-1, mq, -1)
+        seen = torch.gather(bits, 2, m) | (newest < 0)[:, None]
+    seen = (seen & (t < kv_len[:, None])[:, None])[:, :, None].expand(-1, -1, heads, -1).flatten(1, 2)
+    out, lse = softmax_products(score, seen, rows[..., :c["rank"]])
+    # [seqs, mq * heads, ...] back to the rows of q
+    r = torch.arange(total, device=q.device)
+    b = (cu[1:, None] <= r).sum(0)
+    out = out.unflatten(1, (mq, heads))[b, r - cu[b]]
+    return {"out": out.to(q.dtype), "lse": lse.unflatten(1, (mq, heads))[b, r - cu[b]]}
+
+
+def prompt(s):
+    c, q, cu_q, cu_k = s["case"], s["q"], s["cu_q"].long(), s["cu_k"].long()
+    mq, mk = s["max_q"], s["max_k"]
+    nq, nk = cu_q[1:] - cu_q[:-1], cu_k[1:] - cu_k[:-1]
+    i, t = torch.arange(mq, device=q.device), torch.arange(mk, device=q.device)
+    at_q = (cu_q[:-1, None] + i).clamp(max=q.shape[0] - 1)
+    at_k = (cu_k[:-1, None] + t).clamp(max=s["k"].shape[0] - 1)
+    x = q.float()[at_q].transpose(1, 2)                                  # [seqs, heads, mq, dim]
+    shared = s["k_rot"].float()[:, None].expand(-1, s["k"].shape[1], -1)
+    keys = torch.cat([s["k"].float(), shared], -1)[at_k].transpose(1, 2).repeat_interleave(c["group"], 1)
+    v = s["v"].float()[at_k].transpose(1, 2).repeat_interleave(c["group"], 1)
+    score = torch.matmul(x, keys.transpose(2, 3)).mul_((c["nope"] + c["rot"]) ** -0.5)
+    seen = (t < nk[:, None])[:, None]
+    if c["causal"]:   # aligned at the end
+        seen = seen & (t <= (nk - nq)[:, None, None] + i[:, None])
+    out, lse = softmax_products(score, seen[:, None], v)
+    r = torch.arange(q.shape[0], device=q.device)
+    b = (cu_q[1:, None] <= r).sum(0)
+    out, lse = out.transpose(1, 2)[b, r - cu_q[b]], lse.transpose(1, 2)[b, r - cu_q[b]]
+    return {"out": out.to(q.dtype), "lse": lse}
+
+
+def fork(refs, table, kv_len, parent, page):
+    """Rows with a parent take its length and its pages, which they then hold too."""
+    child = parent >= 0
+    of = parent.clamp(min=0).long()
+    kv_len.copy_(torch.where(child, kv_len[of], kv_len))
+    entry = torch.arange(table.shape[1], device=table.device)
+    held = child[:, None] & (entry < ((kv_len + page - 1) // page)[:, None])
+    table.copy_(torch.where(held, table[of], table))
+    refs += torch.bincount(table[held], minlength=len(refs))
+
+
+def resize(refs, table, kv_len, new_len, page):
+    """Rows to new lengths (below 0: as they are): the lowest free pages in the order of rows, a shared
+    last page that is grown into exchanged for one of its own, pages that are not needed given back.
+    Returns the pages to copy of each row, or -1."""
+    new = torch.where(new_len < 0, kv_len, new_len).long()
+    have, need = (kv_len.long() + page - 1) // page, (new + page - 1) // page
+    last = table.gather(1, (have - 1).clamp(min=0)[:, None])[:, 0].clamp(min=0)
+    own_page = (new > kv_len) & (kv_len % page != 0) & (refs[last.long()] > 1)
+    take = (need - have).clamp(min=0) + own_page
+    start = take.cumsum(0) - take
+    free = (refs == 0).nonzero()[:, 0].int()
+    fits = start + take <= len(free)
+    take, own_page = torch.where(fits, take, 0), own_page & fits
+    new, need = torch.where(fits, new, kv_len), torch.where(fits, need, have)
+    entry = torch.arange(table.shape[1], device=table.device)
+    back = (entry >= need[:, None]) & (entry < have[:, None])
+    refs -= torch.bincount(torch.cat([table[back], last[own_page]]), minlength=len(refs))
+    table.masked_fill_(back, -1)
+    first = have - own_page.long()
+    got = (entry >= first[:, None]) & (entry < (first + take)[:, None])
+    pages = free[(start[:, None] + entry - first[:, None]).clamp(0, len(free) - 1)]
+    table.copy_(torch.where(got, pages, table))
+    refs += torch.bincount(table[got], minlength=len(refs))
+    kv_len.copy_(new)
+    dst = table.gather(1, (have - 1).clamp(min=0)[:, None])[:, 0]
+    return torch.where(own_page[:, None], torch.stack([last, dst], 1), -1)
+
+
+def compact(refs, table, kv_len, page):
+    """The highest pages in use into the lowest holes, until none is above one. Returns the moves, -1 from
+    their end on, and how many pages are in use."""
+    n = len(refs)
+    used = refs > 0
+    count = used.sum()
+    at = torch.arange(n, device=refs.device)
+    moves = torch.full((n, 2), -1, dtype=torch.int32, device=refs.device)
+    src = (used & (at >= count)).nonzero()[:, 0].flip(0)
+    dst = (~used & (at < count)).nonzero()[:, 0]
+    moves[:len(src), 0], moves[:len(src), 1] = src.int(), dst.int()
+    to = at.int()
+    to[src] = dst.int()
+    entry = torch.arange(table.shape[1], device=table.device)
+    held = entry < ((kv_len + page - 1) // page)[:, None]
+    table.copy_(torch.where(held, to[table.clamp(min=0).long()], table))
+    refs[dst] = refs[src]
+    refs[src] = 0
+    return moves, count[None].int()
+
+
+def copy_pages(caches, pairs):
+    pairs = pairs[pairs[:, 0] >= 0].long()
+    for x in sum(caches, []):
+        x[pairs[:, 1]] = x[pairs[:, 0]]
+
+
+def run_pages(s):
+    c, kvr = s["case"], None
+    if own:
+        import paper_2608_30830_amd as kvr
+    if c["kind"] == "branch":
+        refs, table, kv_len, page = s["refs"], s["page_table"], s["kv_len"], c["page"]
+        if own:
+            kvr.kvr_pages_resize(refs, table, kv_len, s["ended"], page, check=False)
+            kvr.kvr_pages_fork(refs, table, kv_len, s["parent"], page, check=False)
+            pairs = kvr.kvr_pages_resize(refs, table, kv_len, s["grown"], page, check=False)
+            kvr.kvr_pages_copy(s["buffers"], pairs, check=False)
+        else:   # the branches of before end, new ones begin and grow
+            resize(refs, table, kv_len, s["ended"], page)
+            fork(refs, table, kv_len, s["parent"], page)
+            pairs = resize(refs, table, kv_len, s["grown"], page)
+            copy_pages(s["caches"], pairs)
+        return {"refs": refs, "page_table": table, "kv_len": kv_len, "pairs": pairs, "caches": s["caches"]}
+    refs, table = s["refs"].clone(), s["page_table"].clone()
+    if own:
+        moves, count = kvr.kvr_pages_compact(refs, table, s["kv_len"], c["page"], check=False)
+        kvr.kvr_pages_copy(s["buffers"], moves, check=False)
+    else:
+        moves, count = compact(refs, table, s["kv_len"], c["page"])
+        copy_pages(s["caches"], moves)
+    return {"refs": refs, "page_table": table, "moves": moves, "used": count, "caches": s["caches"]}
+
+
+def run(state):
+    s, c = state, state["case"]
+    if c["op"] == "pages":
+        return run_pages(s)
+    if not own:
+        return {"write": write, "attention": attend, "prompt": prompt}[c["op"]](s)
+    import paper_2608_30830_amd as kvr
+    if c["op"] == "write":
+        kvr.kvr_latent_write(s["handle"], s["latent"], s["key"], s["slots"], s["positions"], s["table"],
+                             norm_weight=s["weight"], eps=EPS, interleaved=c["interleaved"], check=False)
+        return kvr.kvr_latent_read(s["handle"], s["slots"], DTYPES[c["dtype"]], check=False)
+    if c["op"] == "attention":
+        out, lse = kvr.kvr_latent_attention(s["handle"], s["q"], s["cu_q"], s["kv_len"], s["page_table"],
+                                            s["max_q"], s["max_kv"], s["scale"], tree_mask=s["mask"],
+                                            want_lse=True, check=False)
+    else:
+        out, lse = kvr.kvr_latent_prompt(s["q"], s["k"], s["k_rot"], s["v"], s["cu_q"], s["cu_k"],
+                                         s["max_q"], s["max_k"], causal=c["causal"], want_lse=True,
+                                         check=False)
+    return {"out": out, "lse": lse}
+
+
+# ---- the definitions in 64 bits -----------------------------------------------------------------
+
+def power64(k):
+    """2^k exactly, for whole k in the range of normal numbers."""
+    return ((k.long() + 1023) << 52).view(torch.float64)
+
+
+def quantised64(x):
+    """The values that blocks of 32 keep: each rounded to the format's spacing at its own magnitude,
+    halves to the even multiple."""
+    blocks = x.reshape(x.shape[:-1] + (-1, 32))
+    most = blocks.abs().amax(-1, keepdim=True)
+    k = torch.ceil(torch.log2(most.clamp(min=1e-300) / LARGEST)).clamp(min=-900)
+    k = torch.where(most > LARGEST * power64(k), k + 1, k)
+    k = torch.where(most <= LARGEST * power64(k - 1), k - 1, k).clamp(min=MIN_EXP)
+    y = blocks / power64(k)
+    step = power64((torch.frexp(y.abs())[1] - 1).clamp(min=-6) - 3)
+    return (torch.round(y / step) * step * power64(k)).reshape(x.shape)
+
+
+def dequantised64(rows, scale):
+    if scale is None:
+        return rows.double()
+    code = rows.int()
+    e, m = (code >> 3) & 15, code & 7
+    y = torch.where(e == 0, m / 8.0 * 2.0 ** -6, (1 + m / 8.0) * power64(e - 7))
+    return torch.where(code >= 128, -y, y) * power64(scale.long() - 127).repeat_interleave(32, -1)
+
+
+def softmax64(e, v):
+    """Rows of scores, hidden ones -infinity, and values."""
+    total = torch.logsumexp(e, -1)
+    p = torch.exp(e - torch.where(total > -math.inf, total, 0.0)[:, None])
+    return p @ v, total
+
+
+def exact(case, seed):
+    if case["op"] == "pages":
+        return exact_pages(case, seed)
+    s, c = prepare(case, seed), case
+    if c["op"] == "write":
+        x = s["latent"].double()
+        if c["norm"]:
+            x = s["weight"].double() * x / (x.pow(2).mean(1, keepdim=True) + EPS).sqrt()
+        t = s["table"].double()[s["positions"].long()]
+        key = s["key"].double()
+        pairs = key.reshape(len(key), -1, 2) if c["interleaved"] else \
+            key.reshape(len(key), 2, -1).transpose(1, 2)
+        z = torch.complex(pairs[..., 0], pairs[..., 1]) * torch.complex(t[:, 0], t[:, 1])
+        turned = torch.view_as_real(z) if c["interleaved"] else torch.view_as_real(z).transpose(1, 2)
+        x = torch.cat([x, turned.reshape(key.shape)], 1)
+        if c["fmt"] == "fp8":
+            x = quantised64(x)
+        x[s["slots"] < 0] = 0.0
+        return x
+    kv, nq = lengths(c)
+    q = s["q"].double()
+    lse = q.new_zeros(q.shape[:2])
+    if c["op"] == "prompt":
+        if sum(n * t for t, n in zip(kv, nq)) * c["heads"] * c["group"] > 3 * 10 ** 9:
+            return None
+        out, q0, k0 = q.new_zeros(q.shape[:2] + (c["nope"],)), 0, 0
+        for t, n in zip(kv, nq):
+            hidden = torch.zeros(n, t, dtype=torch.bool, device="cuda")
+            if c["causal"]:
+                hidden = torch.ones_like(hidden).triu(t - n + 1)
+            for h in range(q.shape[1]):
+                x = q[q0:q0 + n, h]
+                kv_head = h // c["group"]
+                e = x[:, :c["nope"]] @ s["k"][k0:k0 + t, kv_head].double().T.contiguous()
+                e += x[:, c["nope"]:] @ s["k_rot"][k0:k0 + t].double().T.contiguous()
+                e = (e / math.sqrt(q.shape[2])).masked_fill(hidden, -math.inf)
+                out[q0:q0 + n, h], lse[q0:q0 + n, h] = softmax64(e, s["v"][k0:k0 + t, kv_head].double())
+            q0, k0 = q0 + n, k0 + t
+        return {"out": out, "lse": lse}
+    out, first = q.new_zeros(q.shape[:2] + (c["rank"],)), 0
+    for b, (t, n) in enumerate(zip(kv, nq)):
+        pages = s["page_table"][b, :-(-t // c["page"])].long()
+        scale = s["cache"]["scale"]
+        rows = dequantised64(s["cache"]["rows"][pages], None if scale is None else scale[pages])
+        rows = rows.reshape(-1, rows.shape[-1])[:t]
+        seen = torch.ones(n, t, dtype=torch.bool, device="cuda")
+        if s["mask"] is None:
+            seen[:, t - n:] = torch.tril(seen[:, t - n:])
+        else:
+            word = s["mask"][first:first + n]
+            seen[:, t - n:] = ((word >> torch.arange(n, device="cuda")) & 1).bool()
+        for i in range(n):
+            e = (q[first + i] @ rows.T.contiguous() * s["scale"]).masked_fill(~seen[i], -math.inf)
+            out[first + i], lse[first + i] = softmax64(e, rows[:, :c["rank"]])
+        first += n
+    return {"out": out, "lse": lse}
+
+
+def exact_pages(case, seed):
+    """What the pages of the caches hold: whole numbers have no value of their own here."""
+    s, c = prepare(case, seed), case
+    page, lens = c["page"], lengths(c)[0]
+    held = set(s["page_table"][s["page_table"] >= 0].tolist())
+    n = len(s["refs"])
+    free = [p for p in range(n) if p not in held]
+    moved = []
+    if c["kind"] == "branch":   # branches in order; each last page in part is shared, by all its branches
+        for i, length in enumerate(lens):
+            for _ in range(c["branches"]):
+                if length % page:
+                    moved.append((int(s["page_table"][i, length // page]), free[0]))
+                free = free[-(-(length + c["grow"]) // page) - length // page:]
+    else:
+        moved = list(zip(sorted((p for p in held if p >= len(held)), reverse=True), free))
+    out = [[x.double() for x in layer] for layer in s["caches"]]
+    for src, dst in moved:
+        for layer in out:
+            for x in layer:
+                x[dst] = x[src]
+    names = ("refs", "page_table", "kv_len", "pairs") if c["kind"] == "branch" else \
+        ("refs", "page_table", "moves", "used")
+    return dict({x: None for x in names}, caches=out)

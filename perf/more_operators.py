@@ -465,7 +465,7 @@ def resize(refs, table, kv_len, new_len, page):
     take = (need - have).clamp(min=0) + own_page
     start = take.cumsum(0) - take
     free = (refs == 0).nonzero()[:, 0].int()
-    fits = start + take <= len(free)
+    fits = (take == 0) | (start + take <= len(free))
     take, own_page = torch.where(fits, take, 0), own_page & fits
     new, need = torch.where(fits, new, kv_len), torch.where(fits, need, have)
     entry = torch.arange(table.shape[1], device=table.device)

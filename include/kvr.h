@@ -551,6 +551,190 @@ int kvr_tree_attention(const kvr_kv_cache *cache, const kvr_sequences *seqs, con
                        float *d_lse, int32_t *d_status, void *d_ws, size_t *ws_bytes,
                        void *hip_stream);
 
+/* ---- The latent cache ---------------------------------------------------------
+ * One row a token for all heads: `rank` elements from which every head's key and value
+ * follow by a product with a weight, and `rot` elements of a key that all heads share and
+ * that carries the position.  Formats KVR_KV_BF16, KVR_KV_FP16 and KVR_KV_FP8 (blocks of 32
+ * with a scale byte as above; the last blocks are those of the shared key); pages, slots,
+ * device-detected errors and the other conventions are those of the cache above. */
+typedef struct {
+    void *data;                 /* device, 16-byte aligned                            */
+    void *scale;                /* device, scale bytes; NULL for 16-bit formats       */
+    int64_t page_stride, token_stride;              /* bytes, of 16                   */
+    int64_t scale_page_stride, scale_token_stride;  /* bytes                          */
+    int64_t n_pages;            /* 1 .. 2^31 - 1                                      */
+    int32_t page_size;          /* tokens: a power of two, 16 .. 32,768               */
+    int32_t rank;               /* 256 or 512                                         */
+    int32_t rot;                /* 32 or 64                                           */
+    int32_t format;             /* KVR_KV_BF16, KVR_KV_FP16 or KVR_KV_FP8             */
+} kvr_latent_cache;             /* token_stride and scale_token_stride: at most 2^26  */
+
+/*
+ * Writes rows of the latent cache: latents, with d_norm normalised to
+ *   c_i w_i / sqrt(mean(c^2) + eps),
+ * and shared keys, rotated as in kvr_cache_write; both in 32 bits and rounded once, by
+ * the cache's format.
+ *   d_latent       device, dtype [n_tokens][rank], stride in elements, 16-byte aligned rows.
+ *   d_key          device, dtype [n_tokens][rot], likewise.
+ *   d_norm         device, dtype [rank], 16-byte aligned, or NULL (latents as they are);
+ *                  eps finite and >= 0 (else KVR_E_GRID).
+ *   d_slots, d_pos, d_table, n_pos, rot_dim, flags: as kvr_cache_write, rot_dim <= rot.
+ */
+int kvr_latent_write(const kvr_latent_cache *cache, const void *d_latent, const void *d_key,
+                     int32_t dtype, int64_t n_tokens, int64_t latent_stride, int64_t key_stride,
+                     const void *d_norm, float eps, const int64_t *d_slots, const int32_t *d_pos,
+                     const float *d_table, int64_t n_pos, int32_t rot_dim, int32_t flags,
+                     int32_t *d_status, void *hip_stream);
+
+/*
+ * Reads rows of the latent cache back: d_out [n_tokens][rank + rot] in dtype (stride in
+ * elements, 16-byte aligned rows) from slots as kvr_cache_read takes them.
+ */
+int kvr_latent_read(const kvr_latent_cache *cache, const int64_t *d_slots, int64_t n_tokens,
+                    void *d_out, int32_t dtype, int64_t out_stride, int32_t *d_status,
+                    void *hip_stream);
+
+/*
+ * Attention of each sequence's newest tokens over its pages of the latent cache, in the
+ * latent's space (the absorbed form): with rows x_j of rank + rot elements,
+ *   out[i][h] = sum_j softmax_j(scale * q[i][h] . x_j) x_j[: rank],  lse[i][h] = log of the sum,
+ * where q[i][h] is head h's query times its key weight, beside its rotated part.  Sequences,
+ * what each query sees, masks, hidden and unwritten rows, errors and the workspace are those
+ * of kvr_tree_attention.  An element of a latent that a query sees and that is an infinity
+ * or a NaN gives NaN.
+ *   d_q            device, dtype [n_queries][n_heads][rank + rot]; KVR_DT_BF16, or
+ *                  KVR_DT_FP16 with a KVR_KV_FP16 cache (which takes no other).
+ *   d_out          device, dtype [n_queries][n_heads][rank], no overlap with d_q.
+ *   d_lse          device, float32 [n_queries][n_heads] or NULL.
+ *   Sizes: max_q * n_heads <= 2^24, max_kv <= 2^30.
+ */
+int kvr_latent_attention(const kvr_latent_cache *cache, const kvr_sequences *seqs, const void *d_q,
+                         int32_t dtype, int32_t n_heads, int64_t q_token_stride,
+                         int64_t q_head_stride, const uint64_t *d_tree_mask, int32_t mask_words,
+                         float scale, void *d_out, int64_t out_token_stride,
+                         int64_t out_head_stride, float *d_lse, int32_t *d_status, void *d_ws,
+                         size_t *ws_bytes, void *hip_stream);
+
+/* A kvr_latent_prompt call's shape. */
+typedef struct {
+    const int32_t *d_cu_q;      /* device [n_seqs + 1]: first query of each sequence, then n_queries */
+    const int32_t *d_cu_k;      /* device [n_seqs + 1]: first key of each sequence, then n_keys      */
+    int64_t n_queries, n_keys;  /* of all sequences, <= 2^31 - 1                                     */
+    int32_t n_seqs;             /* 0 .. 4,096                                                        */
+    int32_t max_q, max_k;       /* bounds on a sequence's queries and keys, >= 1; max_k <= 2^30      */
+    int32_t n_q_heads;          /* a multiple of n_kv_heads                                          */
+    int32_t n_kv_heads;         /* 1 .. 1,024                                                        */
+    int32_t nope;               /* elements of a head's own key, and of its value: 64 or 128         */
+    int32_t rot;                /* elements of the key that all heads share: 32 or 64                */
+    int32_t causal;             /* 1: query i of n sees the keys up to its own, the last n keys      *
+                                 * being the queries' (key j of m where j <= m - n + i); 0: all      */
+} kvr_prompt;
+
+/*
+ * Attention of prompts, or of their next chunks, with keys and values expanded from the latents
+ * for each head and the rotated part that all heads share:
+ *   s_ij = scale (q[i][h][: nope] . k[j][h'] + q[i][h][nope :] . k_rot[j]),
+ *   out[i][h] = sum_j softmax_j(s_ij) v[j][h'],  lse[i][h] = log of the sum,
+ * h' = h / (n_q_heads / n_kv_heads).  A query that sees nothing gets zeros and -infinity; keys and
+ * values that it does not see, NaN and infinities included, do not reach it.  A value that it sees
+ * and that is an infinity gives an infinity or NaN.
+ *   d_q            device, dtype (KVR_DT_BF16 or KVR_DT_FP16) [n_queries][n_q_heads][nope + rot].
+ *   d_k, d_v       device, dtype [n_keys][n_kv_heads][nope]; token strides up to 2^24 elements.
+ *   d_k_rot        device, dtype [n_keys][rot], stride likewise.
+ *   d_out          device, dtype [n_queries][n_q_heads][nope], no overlap with the inputs.
+ *   d_lse          device, float32 [n_queries][n_q_heads] or NULL.
+ *   Strides in elements, 16-byte aligned rows.  Scores, the softmax and the sums are held in
+ *   float32; the weights are rounded to dtype for their product.
+ *   A sequence whose lengths do not fit the call (beyond max_q or max_k, or beyond n_queries or
+ *   n_keys) is left out: KVR_E_DOMAIN.  Where d_cu_q decreases, any sequence may be left out.
+ *   d_ws, ws_bytes as kvr_tree_attention.
+ *   Sizes: n_q_heads <= 4,096, max_q * n_q_heads <= 2^30, n_queries * n_q_heads <= 2^36.
+ */
+int kvr_latent_prompt(const kvr_prompt *prompt, const void *d_q, int32_t dtype,
+                      int64_t q_token_stride, int64_t q_head_stride, const void *d_k,
+                      int64_t k_token_stride, int64_t k_head_stride, const void *d_k_rot,
+                      int64_t k_rot_stride, const void *d_v, int64_t v_token_stride,
+                      int64_t v_head_stride, float scale, void *d_out, int64_t out_token_stride,
+                      int64_t out_head_stride, float *d_lse, int32_t *d_status, void *d_ws,
+                      size_t *ws_bytes, void *hip_stream);
+
+/* ---- The pages of a cache ------------------------------------------------------
+ * One pool of pages, shared by the caches of all layers (of either kind): d_refs, device
+ * int32 [n_pages], counts the rows that hold each page (0: free).  Row b of the page table,
+ * device int32 [n_seqs][pages_stride], holds the pages of its kv_len[b] tokens in order, the
+ * first ceil(kv_len / page_size) entries; the others have no meaning and are left as they are.
+ * The calls below keep refs, table and lengths in step, work in place, and give the same
+ * results whenever they start from the same state.  A row that does not fit a call (a length
+ * below 0 or beyond max_pages entries, where it must not be; an entry outside the pool) is
+ * reported as KVR_E_DOMAIN; so is a page that is given back more often than it was held. */
+typedef struct {
+    int32_t *d_refs;            /* device [n_pages]                                   */
+    int32_t *d_pages;           /* device [n_seqs][pages_stride]                      */
+    int32_t *d_kv_len;          /* device [n_seqs]                                    */
+    int64_t n_pages;            /* 1 .. 2^30                                          */
+    int64_t pages_stride;       /* elements between rows                              */
+    int32_t max_pages;          /* entries of a row, 0 .. 2^24                        */
+    int32_t n_seqs;             /* 0 .. 65,536                                        */
+    int32_t page_size;          /* tokens: a power of two, 16 .. 32,768               */
+} kvr_page_pool;
+
+/*
+ * Branches: row b with a parent a = d_parent[b] >= 0 takes a's length and pages, which it then
+ * holds too, the last, partly filled one included (kvr_pages_resize copies it before either
+ * grows into it).  b must be empty and a must be another row without a parent, else row b is
+ * left as it is: KVR_E_DOMAIN.
+ *   d_parent       device, int32 [n_seqs]; below 0: the row stays as it is.
+ */
+int kvr_pages_fork(const kvr_page_pool *pool, const int32_t *d_parent, int32_t *d_status,
+                   void *hip_stream);
+
+/*
+ * New lengths of rows: new[b] below 0 leaves row b as it is, more tokens take pages, fewer (0
+ * among them) give pages back, their entries set to -1.  Pages are taken lowest first, in the
+ * order of rows and of their entries, from those that are free when the call begins.  A row
+ * that grows and whose last page is partly filled and held by other rows too takes a page in
+ * its place: d_copies[b] = (that page, the row's new one), to be copied by kvr_pages_copy
+ * before the row is written to; else (-1, -1).  A row that needs pages, where those that it and
+ * the rows before it need exceed the free ones, does not grow: KVR_E_DOMAIN, and its length stays.
+ *   d_new_len      device, int32 [n_seqs].
+ *   d_copies       device, int32 [n_seqs][2].
+ *   d_ws, ws_bytes workspace (two-phase sizing; contents need not be set).
+ */
+int kvr_pages_resize(const kvr_page_pool *pool, const int32_t *d_new_len, int32_t *d_copies,
+                     int32_t *d_status, void *d_ws, size_t *ws_bytes, void *hip_stream);
+
+/*
+ * Brings the pages in use together: the highest one moves into the lowest free one while that
+ * is lower, at most max_moves times; refs and tables follow.  d_moves[k] = (from, to) of move k,
+ * to be copied by kvr_pages_copy, and (-1, -1) from the last one on.
+ *   d_moves        device, int32 [max_moves][2]; max_moves 0 .. n_pages.
+ *   d_used         device, int32 [1]: pages in use (with all moves done, those below it).
+ *   Pages that are in use but in no row of the table move too.
+ */
+int kvr_pages_compact(const kvr_page_pool *pool, int32_t *d_moves, int64_t max_moves,
+                      int32_t *d_used, int32_t *d_status, void *d_ws, size_t *ws_bytes,
+                      void *hip_stream);
+
+/* What a page is of one tensor of a cache: `outer` x `inner` runs of `run_bytes` bytes. */
+typedef struct {
+    void *data;                 /* device: the first page                             */
+    int64_t page_stride;        /* bytes, >= 0                                        */
+    int64_t outer_stride, inner_stride;  /* bytes, >= 0                               */
+    int64_t run_bytes;          /* >= 1; outer * inner * run_bytes <= 2^40            */
+    int32_t outer, inner;       /* >= 1                                               */
+} kvr_page_buffer;
+
+/*
+ * Copies pages in any number of tensors: page d_pairs[i][0] to page d_pairs[i][1].  Pairs with
+ * a number below 0 are left out, those outside the pool too: KVR_E_DOMAIN.  No page may be
+ * written twice, or written and read, in one call.
+ *   buffers        host, [n_buffers].
+ *   d_pairs        device, int32 [n_pairs][2].
+ *   Sizes: n_buffers <= 65,536, n_pairs <= 2^30, n_pages <= 2^31 - 1.
+ */
+int kvr_pages_copy(const kvr_page_buffer *buffers, int32_t n_buffers, int64_t n_pages,
+                   const int32_t *d_pairs, int64_t n_pairs, int32_t *d_status, void *hip_stream);
+
 /*
  * Instrumentation for benchmarks.  After this call, every kvr_cost_grid,
  * kvr_cost_grid_noalloc, kvr_bootstrap, kvr_bootstrap_factored,

@@ -12,12 +12,16 @@ import math
 import os
 from typing import Optional, Sequence, Tuple
 
-from . import kv
+from . import kv, latent, pages
 from .kv import (KVR_DT_BF16, KVR_DT_FP16, KVR_DT_FP32, KVR_KV_BF16, KVR_KV_FP16,  # noqa: F401
                  KVR_KV_FP4, KVR_KV_FP8, KVR_ROPE_BASE, KVR_ROPE_INDEX, KVR_ROPE_LINEAR,
                  KVR_ROPE_PLAIN, KVR_ROPE_TURNS, KVR_ROTARY_ADJOINT, KVR_ROTARY_INTERLEAVED,
                  KvCache, kv_bytes_per_token, kvr_cache_read, kvr_cache_write, kvr_kv_cache,
                  kvr_rope, kvr_rotary, kvr_rotary_table, kvr_sequences, kvr_tree_attention)
+from .latent import (LatentCache, kvr_latent_attention, kvr_latent_cache, kvr_latent_prompt,  # noqa: F401
+                     kvr_latent_read, kvr_latent_write, kvr_prompt, latent_bytes_per_token)
+from .pages import (PageBuffers, kvr_page_buffer, kvr_page_pool, kvr_pages_compact,  # noqa: F401
+                    kvr_pages_copy, kvr_pages_fork, kvr_pages_resize)
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 # KVR_LIBRARY names another build of the same library (e.g. one whose host
@@ -43,7 +47,7 @@ EXPORTS = ("kvr_prices_from_platform", "kvr_cost_grid", "kvr_cost_grid_noalloc",
            "kvr_select_policy", "kvr_bootstrap",
            "kvr_bootstrap_factored", "kvr_eq3_timer", "kvr_capacity_replay",
            "kvr_controller_select", "kvr_crossover_statistic", "kvr_workspace_status",
-           "kvr_set_profile_events", "kvr_status_string") + kv.EXPORTS
+           "kvr_set_profile_events", "kvr_status_string") + kv.EXPORTS + latent.EXPORTS + pages.EXPORTS
 
 
 class kvr_prices(ctypes.Structure):
@@ -120,6 +124,8 @@ def load_library(path: str = LIB_PATH):
     lib.kvr_status_string.argtypes = [ctypes.c_int]
     lib.kvr_status_string.restype = ctypes.c_char_p
     kv.declare(lib)
+    latent.declare(lib)
+    pages.declare(lib)
     _lib = lib
     return lib
 

@@ -23,9 +23,16 @@ SOURCES = ["kvr_api.cpp", "kvr_grid.hip", "kvr_aux.hip", "kvr_sorted.hip", "kvr_
            "kvr_factored.hip", "kvr_noalloc.hip", "kvr_small.hip",
            "kvr_kv_api.cpp", "kvr_rotary.hip", "kvr_cache.hip", "kvr_attention.hip",
            "kvr_attention_bf16.hip", "kvr_attention_fp16.hip", "kvr_attention_fp8.hip",
-           "kvr_attention_fp8h.hip", "kvr_attention_fp4.hip", "kvr_attention_fp4h.hip"]
+           "kvr_attention_fp8h.hip", "kvr_attention_fp4.hip", "kvr_attention_fp4h.hip",
+           "kvr_latent_api.cpp", "kvr_latent.hip", "kvr_latent_cache.hip", "kvr_latent_bf16.hip",
+           "kvr_latent_fp16.hip", "kvr_latent_fp8.hip", "kvr_prompt.hip",
+           "kvr_pages_api.cpp", "kvr_pages.hip"]
 # Kernels that meet whatever a model or unwritten memory holds: NaNs are kept.
-NAN_SAFE = tuple(s for s in SOURCES if s.startswith(("kvr_rotary", "kvr_cache", "kvr_attention")))
+NAN_SAFE = tuple(s for s in SOURCES if s.startswith(("kvr_rotary", "kvr_cache", "kvr_attention",
+                                                     "kvr_latent", "kvr_prompt")))
+# Kernels whose accumulators are more than 256 registers: matrix instructions may then take
+# them from either half of the register file (else hundreds of registers go to memory).
+WIDE = ("kvr_latent_bf16.hip", "kvr_latent_fp16.hip", "kvr_latent_fp8.hip", "kvr_prompt.hip")
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
           # no packed-fp32 instruction selection anywhere
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -38,6 +45,7 @@ DEVICE = ["-Xarch_device", "-fno-honor-nans"]
 def _compile(src: str) -> str:
     obj = os.path.join(OUT_DIR, os.path.basename(src) + ".o")
     cmd = [HIPCC] + COMMON + (DEVICE if src.endswith(".hip") and src not in NAN_SAFE else []) + \
+        (["-mllvm", "-amdgpu-mfma-vgpr-form=1"] if src in WIDE else []) + \
         ["-c", os.path.join(CSRC, src), "-o", obj]
     subprocess.run(cmd, check=True, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
     return obj

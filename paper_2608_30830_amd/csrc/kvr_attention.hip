@@ -125,18 +125,20 @@ hipError_t launch_combine(const Attention &a, hipStream_t stream)
 {
     const int64_t rows = (int64_t)a.max_q * a.group;
     const bool many = rows * a.c.n_heads * a.n_seqs >= 4096;
-    const bool narrow = a.c.dim <= 128;
+    const bool narrow = a.c.dim <= 128, latent = a.c.dim == 512;   // (256 and 512: also a latent's)
     // Many parts of few sequences: a block of 1,024 (one sequence of 90,196 tokens in 4 bits and
     // one KV head, 470 parts: 24.5 -> 18.7 us a call; with 96 parts of 56 rows 73 -> 75).
     const int64_t parts = std::min<int64_t>(a.target / a.n_seqs, cdiv(a.max_kv, kStep) / a.min_steps);
     const bool deep = !many && parts > 128;
     const int threads = deep ? 1024 : 256;
-    const int groups = many ? 1 : (narrow ? 8 : 4) * (threads / 256);   // at most all lanes a row
+    const int groups = many ? 1 : (narrow ? 8 : latent ? 2 : 4) * (threads / 256);   // at most all lanes a row
     const dim3 grid((unsigned)cdiv(rows, threads / (a.c.dim / 4 * groups)), a.c.n_heads, a.n_seqs);
     if (many) combine_kernel<QT, 1, 256><<<grid, 256, 0, stream>>>(a);
     else if (deep && narrow) combine_kernel<QT, 32, 1024><<<grid, 1024, 0, stream>>>(a);
+    else if (deep && latent) combine_kernel<QT, 8, 1024><<<grid, 1024, 0, stream>>>(a);
     else if (deep) combine_kernel<QT, 16, 1024><<<grid, 1024, 0, stream>>>(a);
     else if (narrow) combine_kernel<QT, 8, 256><<<grid, 256, 0, stream>>>(a);
+    else if (latent) combine_kernel<QT, 2, 256><<<grid, 256, 0, stream>>>(a);
     else combine_kernel<QT, 4, 256><<<grid, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
@@ -206,6 +208,12 @@ size_t plan_attention(Attention &a)
     return (size_t)a.max_items * a.c.n_heads * a.block_rows * (a.c.dim + 4) * sizeof(float);
 }
 
+hipError_t launch_join(const Attention &a, hipStream_t stream)
+{
+    return a.q.dtype == KVR_DT_FP16 ? launch_combine<KVR_DT_FP16>(a, stream)
+                                    : launch_combine<KVR_DT_BF16>(a, stream);
+}
+
 hipError_t launch_attention(const Attention &a, hipStream_t stream)
 {
     const dim3 grid((unsigned)((int64_t)a.max_items * a.c.n_heads));
@@ -221,7 +229,7 @@ hipError_t launch_attention(const Attention &a, hipStream_t stream)
         e = half ? launch_attention_fp4h(a, grid, stream) : launch_attention_fp4(a, grid, stream);
     }
     if (e != hipSuccess || a.part_o == nullptr) return e;
-    return half ? launch_combine<KVR_DT_FP16>(a, stream) : launch_combine<KVR_DT_BF16>(a, stream);
+    return launch_join(a, stream);
 }
 
 }  // namespace kv

@@ -111,6 +111,8 @@ struct Attention {
 // Fills the launch plan; returns the workspace bytes (0: no sequence is cut).
 size_t plan_attention(Attention &a);
 hipError_t launch_attention(const Attention &a, hipStream_t stream);
+// Joins the parts that a call's workspace holds.
+hipError_t launch_join(const Attention &a, hipStream_t stream);
 // The attention kernel by cache format and query type.
 hipError_t launch_attention_bf16(const Attention &a, dim3 grid, hipStream_t stream);
 hipError_t launch_attention_fp16(const Attention &a, dim3 grid, hipStream_t stream);

@@ -1,0 +1,68 @@
+// Internal declarations of the pages of a cache: branches, lengths, compaction, copies.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "kvr.h"
+#include "kvr_kv.h"
+
+namespace kvr {
+namespace pages {
+
+constexpr int kChunkWords = 128;                // words of 64 pages that one block counts
+constexpr int kChunk = 64 * kChunkWords;        // pages
+
+struct Pool {
+    int32_t *refs, *table, *len;
+    int64_t n_pages, stride;
+    int32_t width, n_seqs, shift;               // entries of a row; log2 of the page size
+    int32_t chunks;                             // of kChunk pages
+    int *status;
+};
+
+// What a row of a resize call does.
+struct Row {
+    int64_t start;      // pages that the rows before it take
+    int32_t take;       // pages that it takes
+    int32_t first;      // entry of the first of them
+    int32_t need;       // entries that it holds afterwards
+    int32_t mode;
+};
+
+struct Resize {
+    Pool p;
+    const int32_t *new_len;
+    int32_t *copies;
+    uint64_t *free;     // [chunks * kChunkWords] bits of the pages that are free
+    int32_t *count;     // [chunks] of them
+    Row *rows;          // [n_seqs]
+};
+
+struct Compact {
+    Pool p;
+    int32_t *moves, *used;
+    int64_t max_moves;
+    uint64_t *free;
+    int32_t *count;
+    int32_t *where;     // [n_pages] the move of a page beyond the used ones' number, or -1
+};
+
+constexpr int kBuffers = 64;   // of one launch
+struct Copy {
+    char *data[kBuffers];
+    int64_t page_stride, outer_stride, inner_stride, run;   // bytes
+    int32_t outer, inner, width;                            // width: bytes moved at a time
+    int32_t n_buffers, split;                               // blocks of one page
+    int64_t n_pages, n_pairs;
+    const int32_t *pairs;
+    int *status;
+};
+
+hipError_t launch_fork(const Pool &p, const int32_t *parent, hipStream_t stream);
+hipError_t launch_resize(const Resize &r, hipStream_t stream);
+hipError_t launch_compact(const Compact &c, hipStream_t stream);
+hipError_t launch_copy(const Copy &c, hipStream_t stream);
+
+}  // namespace pages
+}  // namespace kvr

@@ -1,5 +1,6 @@
 // Attention over the latent cache: the launch plan.
 #include <algorithm>
+#include <cmath>
 
 #include "kvr_latent.h"
 
@@ -11,15 +12,16 @@ size_t plan_latent_attention(LatentAttention &l)
     Attention &a = l.a;
     const int64_t rows = (int64_t)a.max_q * a.group;
     const int64_t longest = cdiv(a.max_kv, kStep);
-    a.row_tiles = rows <= 16 ? 1 : 2;
-    const int share = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;   // waves that share cached rows
-    a.shared = share > 1;
-    a.waves = 4;
-    a.block_rows = 16 * a.row_tiles * share;
+    const int share = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;   // tiles of 16 rows a block
+    a.block_rows = 16 * share;
     a.min_steps = 8;
-    a.target = l.c.rank == 512 ? 256 : 512;   // blocks that are resident at once, by LDS
+    // Blocks that are resident at once, by LDS.  Sequences are cut into whole numbers of parts, to
+    // the nearest, so that n of them come to about sqrt(n) / 3 parts more or less than planned,
+    // and one more than there is room for would begin another round.
     const int64_t blocks = std::min<int64_t>((int64_t)a.n_seqs * cdiv(rows, a.block_rows),
                                              a.n_queries * a.group / a.block_rows + a.n_seqs);
+    const int64_t slots = 256;
+    a.target = (int32_t)(slots - (int64_t)std::sqrt((double)std::min(blocks, slots)));
     a.max_items = (int32_t)std::max<int64_t>(
         1, std::min(a.target + blocks, blocks * cdiv(longest, a.min_steps)));
     a.direct = 0;

@@ -90,8 +90,7 @@ struct PromptKernel {
     struct State {
         u32x4 q[RT][NB];
         f32x4 o[RT][VT];
-        float m[RT], l[RT];
-        f32x4 w[RT];
+        float m[RT], l[RT], w[RT];   // reference (log2); this lane's part of the sum of the weights, and as rounded
         int last[RT];    // the last key that the lane's query sees (-1: none)
     };
 
@@ -118,26 +117,32 @@ struct PromptKernel {
     }
 
     // Rows of C chunks of a step into LDS; rows past the sequence's last key read as that one.
-    template <int C>
-    __device__ __forceinline__ void bring(const Rows &from, int64_t head, int first, char *to) const
+    template <int C, bool Whole>
+    __device__ __forceinline__ void bring(const Rows &from, int64_t head, int first, uint32_t to) const
     {
         constexpr int Loads = kKeys * C / 64, PerLoad = 64 / C;   // rows of a load
         const int64_t stride = from.token_stride * 2;
-        const char *base = from.p + (int64_t)(k0 + first) * stride + head * from.head_stride * 2;
-        const int last = nk - 1 - first;
+        const char *base = from.p + uniform((int64_t)(k0 + first) * stride + head * from.head_stride * 2);
 #pragma unroll
         for (int j0 = 0; j0 < Loads; j0 += 4) {
-            const int j = j0 + wave;
-            const int r = j * PerLoad + lane / C;
-            const int c = (lane & (C - 1)) ^ swizzle<C>(r);
-            load_to_lds(base + min(r, last) * stride + c * 16, to + j * 1024);
+            const int j = j0 + wave, r = j * PerLoad + lane / C;
+            const uint32_t c = 16 * ((lane & (C - 1)) ^ swizzle<C>(r));
+            if (Whole)
+                load_to_lds(base + j * PerLoad * stride, lane / C * (uint32_t)stride + c, to + j * 1024);
+            else load_to_lds(base + min(r, nk - 1 - first) * stride + c, to + j * 1024);
         }
     }
-    __device__ __forceinline__ void fetch(int step, char *tile) const
+    template <bool Whole>
+    __device__ __forceinline__ void bring_step(int first, uint32_t tile) const
     {
-        bring<NOPE / 8>(p.k, kvh, step * kKeys, tile);
-        bring<ROT / 8>(p.shared, 0, step * kKeys, tile + OwnBytes);
-        bring<NOPE / 8>(p.v, kvh, step * kKeys, tile + ValuesAt);
+        bring<NOPE / 8, Whole>(p.k, kvh, first, tile);
+        bring<ROT / 8, Whole>(p.shared, 0, first, tile + OwnBytes);
+        bring<NOPE / 8, Whole>(p.v, kvh, first, tile + ValuesAt);
+    }
+    __device__ __forceinline__ void fetch(int step, uint32_t tile) const
+    {
+        if ((step + 1) * kKeys <= nk) bring_step<true>(step * kKeys, tile);
+        else bring_step<false>(step * kKeys, tile);
     }
 
     static constexpr float kBelow = MT == KVR_DT_FP16 ? 7.0f : 0.0f;
@@ -145,7 +150,19 @@ struct PromptKernel {
     // sure: every query of the wave sees every key of the step.
     __device__ __forceinline__ bool compute(int step, bool sure, const char *tile, State &st) const
     {
+        bool odd = false;
+        if (!sure) {   // a weight of zero would not hide an infinity or a NaN
+            u16x2 most = {0, 0};
+#pragma unroll 4
+            for (int i = 0; i < OwnBytes / 1024; ++i) {
+                const u32x4 x = *reinterpret_cast<const u32x4 *>(tile + ValuesAt + i * 1024 + lane * 16);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) keep_most<MT>(x[k], most);
+            }
+            odd = any_odd<MT>(most);
+        }
         f32x4 sc[RT][4];
+        u32x4 pv[RT][2];
         static_for<0, 4 * RT>([&](auto I) {
             sc[decltype(I)::value / 4][decltype(I)::value % 4] = f32x4{0, 0, 0, 0};
         });
@@ -153,8 +170,8 @@ struct PromptKernel {
             constexpr int t = decltype(T)::value;
             static_for<0, NB>([&](auto I) {
                 constexpr int i = decltype(I)::value;
-                const char *at = i < KB ? tile + own_at[i < KB ? i : 0] + t * 16 * NOPE * 2
-                                        : tile + shared_at[i < KB ? 0 : i - KB] + t * 16 * ROT * 2;
+                const char *at = tile + (i < KB ? own_at[i < KB ? i : 0] + t * 16 * NOPE * 2
+                                                : shared_at[i < KB ? 0 : i - KB] + t * 16 * ROT * 2);
                 const u32x4 x = *reinterpret_cast<const u32x4 *>(at);
                 static_for<0, RT>([&](auto R) {
                     constexpr int r = decltype(R)::value;
@@ -193,8 +210,6 @@ struct PromptKernel {
                 st.m[r] = t;
             });
         }
-        constexpr uint32_t one = MT == KVR_DT_BF16 ? 0x3f803f80u : 0x3c003c00u;
-        u32x4 pv[RT][2];
         static_for<0, 2 * RT>([&](auto I) {
             constexpr int r = decltype(I)::value / 2, u = decltype(I)::value % 2;
             const f32x4 s0 = sc[r][2 * u], s1 = sc[r][2 * u + 1];
@@ -204,19 +219,19 @@ struct PromptKernel {
                 x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], p.scale2, -st.m[r]));
             st.l[r] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pv[r][u][i] = pack16<MT>(x[2 * i], x[2 * i + 1]);
-            // the outputs are divided by the sum of the weights as rounded
-            st.w[r] = mfma<MT>(u32x4{one, one, one, one}, pv[r][u], st.w[r]);
+            for (int i = 0; i < 4; ++i) {
+                pv[r][u][i] = pack16<MT>(x[2 * i], x[2 * i + 1]);
+                st.w[r] = add_pair<MT>(pv[r][u][i], st.w[r]);   // what the outputs are divided by
+            }
         });
-        bool odd = false;
         static_for<0, 2 * VT>([&](auto E) {
             constexpr int u = decltype(E)::value / VT, e = decltype(E)::value % VT;
             const char *at = tile + val_at[e] + u * 32 * NOPE * 2;
             const u32x2 lo = read_across(at), hi = read_across(at + 16 * NOPE * 2);
             uint32_t w[4] = {lo[0], lo[1], hi[0], hi[1]};
-            if (!sure) {   // a weight of zero would not hide an infinity or a NaN
+            if (odd) {   // (in registers: another wave may see all these keys)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) odd |= clear_odd2<MT>(w[i]);
+                for (int i = 0; i < 4; ++i) clear_odd2<MT>(w[i]);
             }
             const u32x4 x = {w[0], w[1], w[2], w[3]};
             static_for<0, RT>([&](auto R) {
@@ -254,7 +269,7 @@ struct PromptKernel {
         const Item x = find_item(p, item);
         if (x.b < 0) return;
         kvh = h / p.group;
-        nk = x.nk, k0 = x.k0, q0 = x.q0, nq = x.nq;
+        nk = uniform(x.nk), k0 = uniform(x.k0), q0 = uniform(x.q0), nq = uniform(x.nq);
         const int r0 = x.rb * BlockRows, w0 = r0 + WaveRows * wave;
         const int past = nk - nq;   // query i sees the keys up to past + i
         State st;
@@ -270,7 +285,7 @@ struct PromptKernel {
             });
             st.m[r] = kLowest;
             st.l[r] = 0.0f;
-            st.w[r] = f32x4{0, 0, 0, 0};
+            st.w[r] = 0.0f;
             static_for<0, VT>([&](auto E) { st.o[r][decltype(E)::value] = f32x4{0, 0, 0, 0}; });
         });
         // steps of the block, and of its part; the wave's keys [0, see), all of it to `all`
@@ -280,21 +295,22 @@ struct PromptKernel {
         const int end = (int)((int64_t)steps * (part + 1) / p.parts);
         const int see = w0 < nq ? seen(w0 + WaveRows - 1) : 0, all = w0 < nq ? seen(w0) : 0;
         bool odd = false;
-        if (first < end) fetch(first, lds);
+        const uint32_t lds_at = lds_address(lds);
+        if (first < end) fetch(first, lds_at);
         for (int s = first; s < end; ++s) {
-            wait_loads();
-            __syncthreads();   // the step's rows are there, the other buffer has been read
-            if (s + 1 < end) fetch(s + 1, lds + ((s + 1 - first) & 1) * Tile);
+            wait_loads<0>();
+            block_barrier();   // the step's rows are there, the other buffer has been read
+            if (s + 1 < end) fetch(s + 1, lds_at + ((s + 1 - first) & 1) * Tile);
             if (s * kKeys < see)
                 odd |= compute(s, (s + 1) * kKeys <= all, lds + ((s - first) & 1) * Tile, st);
         }
-        odd = __syncthreads_or(odd);
+        __syncthreads();
+        odd = block_any(odd, reinterpret_cast<uint32_t *>(lds));
         static_for<0, RT>([&](auto R) {
             constexpr int r = decltype(R)::value;
             const int i = w0 + 16 * r + n;
-            const float sum = row_sum(st.l[r]);
+            const float sum = row_sum(st.l[r]), norm = row_sum(st.w[r]);
             if (i >= nq) return;
-            const float norm = st.w[r][0];
             const int64_t cell = ((int64_t)at * p.q_heads + h) * BlockRows + (i - r0);
             static_for<0, VT>([&](auto E) {
                 constexpr int e = decltype(E)::value;

@@ -66,7 +66,7 @@ __device__ __forceinline__ Part find_part(const Attention &a, int item)
     int base = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
         if (b0) x = lane_sequence(a, b0);
-        const int parts = parts_of(x.steps, per);
+        const int parts = parts_of(a, x.steps, per);
         const int upto = wave_incl_scan(parts * x.rbs);
         const uint64_t hit = __ballot(base + upto > item);
         if (hit) {

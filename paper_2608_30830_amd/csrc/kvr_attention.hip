@@ -29,12 +29,12 @@ __global__ __launch_bounds__(Threads) void combine_kernel(Attention a)
     if ((int)blockIdx.x * rows_per_block >= rows) return;
     Lane x = lane_sequence(a, 0);
     const int per = part_steps(a, x);
-    const int parts = parts_of(steps_of(len, nq), per);
+    const int parts = parts_of(a, steps_of(len, nq), per);
     if (parts <= 1) return;
     int64_t base = 0;   // items before this sequence's
     for (int b0 = 0; b0 < b; b0 += 64) {
         if (b0) x = lane_sequence(a, b0);
-        base += wave_total(b0 + lane < b ? parts_of(x.steps, per) * x.rbs : 0);
+        base += wave_total(b0 + lane < b ? parts_of(a, x.steps, per) * x.rbs : 0);
     }
     const int local = threadIdx.x / per_row, rest = threadIdx.x - local * per_row;
     const int grp = rest / cols, c = rest - grp * cols;

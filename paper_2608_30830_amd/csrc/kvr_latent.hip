@@ -1,29 +1,27 @@
 // Attention over the latent cache: the launch plan.
 #include <algorithm>
-#include <cmath>
 
 #include "kvr_latent.h"
 
 namespace kvr {
 namespace kv {
 
+constexpr int kSlots = 256;   // blocks that are resident at once: one on each CU, by LDS
+
 size_t plan_latent_attention(LatentAttention &l)
 {
     Attention &a = l.a;
     const int64_t rows = (int64_t)a.max_q * a.group;
     const int64_t longest = cdiv(a.max_kv, kStep);
-    const int share = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;   // tiles of 16 rows a block
-    a.block_rows = 16 * share;
+    // Registers hold 64 rows of 512 elements a block, or 128 of 256.
+    a.block_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || l.c.rank == 512 ? 64 : 128;
     a.min_steps = 8;
-    // Blocks that are resident at once, by LDS.  Sequences are cut into whole numbers of parts, to
-    // the nearest, so that n of them come to about sqrt(n) / 3 parts more or less than planned,
-    // and one more than there is room for would begin another round.
     const int64_t blocks = std::min<int64_t>((int64_t)a.n_seqs * cdiv(rows, a.block_rows),
                                              a.n_queries * a.group / a.block_rows + a.n_seqs);
-    const int64_t slots = 256;
-    a.target = (int32_t)(slots - (int64_t)std::sqrt((double)std::min(blocks, slots)));
+    a.target = kSlots;
+    a.fit = kSlots;   // a block more than there is room for begins another round
     a.max_items = (int32_t)std::max<int64_t>(
-        1, std::min(a.target + blocks, blocks * cdiv(longest, a.min_steps)));
+        1, std::min(std::max<int64_t>(kSlots, blocks), blocks * cdiv(longest, a.min_steps)));
     a.direct = 0;
     if (longest <= a.min_steps) {
         const int64_t room = cdiv(rows, a.block_rows);

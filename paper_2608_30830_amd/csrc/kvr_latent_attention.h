@@ -715,6 +715,7 @@ struct ManyRows : LatentTile<FMT, RK, RO, 64, WAVES> {
     using T::a, T::n, T::g, T::lane, T::len, T::prefix, T::rows;
     static constexpr int MT = T::MT, NB = T::NB, Waves = WAVES, BlockRows = Waves / 2 * 16 * RT;
     static constexpr int VT = RK;   // value tiles of a wave: half of the columns
+    static constexpr int Group = WAVES == 4 ? 8 : RT == 2 ? 2 : 4;   // fragments, as registers allow
     // LDS: two tiles, the weights that waves exchange, what they say about their references
     static constexpr int WeightsAt = 2 * T::Tile, MaxAt = WeightsAt + Waves * RT * 1024;
     static constexpr int FlagAt = MaxAt + Waves * RT * 16 * 4, LdsBytes = FlagAt + 16;
@@ -815,7 +816,7 @@ struct ManyRows : LatentTile<FMT, RK, RO, 64, WAVES> {
                 o[r][e / 2] = mfma<MT>(x, pv[r][e & 1], o[r][e / 2]);
             });
         };
-        fragments<(WAVES == 8 ? 4 : 8), 2 * NB, 2 * VT>(load, key, middle, val);
+        fragments<Group, 2 * NB, 2 * VT>(load, key, middle, val);
         return odd;
     }
 
@@ -909,7 +910,10 @@ hipError_t launch_latent_rows(const LatentAttention &l, dim3 grid, hipStream_t s
     switch (l.a.block_rows) {   // as plan_latent_attention chose
     case 16: return launch_latent_kernel<FewRows<FMT, RK, RO>>(l, grid, stream);
     case 32: return launch_latent_kernel<ManyRows<FMT, RK, RO, 1, 4>>(l, grid, stream);
-    default: return launch_latent_kernel<ManyRows<FMT, RK, RO, 1, 8>>(l, grid, stream);
+    case 64: return launch_latent_kernel<ManyRows<FMT, RK, RO, 1, 8>>(l, grid, stream);
+    default:
+        if constexpr (RK == 8) return launch_latent_kernel<ManyRows<FMT, RK, RO, 2, 8>>(l, grid, stream);
+        else return hipErrorInvalidValue;
     }
 }
 

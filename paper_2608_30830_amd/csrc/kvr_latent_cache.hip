@@ -6,6 +6,7 @@
 // eight adjacent elements, rank / 8 lanes a latent; a wave of large calls has eight
 // rows, so that their loads are in flight together, and then takes all their shared keys, which
 // fill its lanes, in one pass.
+#include "kvr_dpp.h"
 #include "kvr_latent.h"
 #include "kvr_rows.h"
 
@@ -19,9 +20,16 @@ constexpr int kThreads = 256;
 template <int N>
 __device__ __forceinline__ float lanes_sum(float x)
 {
-#pragma unroll
-    for (int m = 1; m < N; m <<= 1) x += __shfl_xor(x, m);
-    return x;
+    // 16 lanes by moves within their row, then rows 16 and 32 apart
+    x += dpp_move<0xB1, 0xf>(x, 0);   // quads: 1, 0, 3, 2
+    x += dpp_move<0x4E, 0xf>(x, 0);   // 2, 3, 0, 1
+    x += dpp_move<0x141, 0xf>(x, 0);  // mirrored in eight
+    x += dpp_move<0x140, 0xf>(x, 0);  // and in sixteen
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    if (N == 32) return x;
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
 // Where a token's row goes, or nullptr.
@@ -117,10 +125,10 @@ __global__ __launch_bounds__(kThreads) void latent_write_kernel(LatentWrite a)
 template <int DT, int FMT, int ROT, int RANK>
 hipError_t write_tokens(const LatentWrite &a, hipStream_t stream)
 {
-    // eight rows a wave once that still leaves 1,024 waves or more
-    const int t = a.tokens >= 8 * 1024 ? 8 : 1;
+    // four rows a wave once that still leaves 2,048 waves or more
+    const int t = a.tokens >= 4 * 2048 ? 4 : 1;
     const dim3 grid = grid_of(cdiv(a.tokens, (kThreads / 64) * t));
-    if (t == 8) latent_write_kernel<DT, FMT, ROT, RANK, 8><<<grid, kThreads, 0, stream>>>(a);
+    if (t == 4) latent_write_kernel<DT, FMT, ROT, RANK, 4><<<grid, kThreads, 0, stream>>>(a);
     else latent_write_kernel<DT, FMT, ROT, RANK, 1><<<grid, kThreads, 0, stream>>>(a);
     return hipGetLastError();
 }

@@ -77,6 +77,28 @@ __host__ __device__ __forceinline__ int part_size(const Attention &a, int64_t to
     const int per = n < (double)longest ? (int)n : longest;
     return per > a.min_steps ? per : a.min_steps;
 }
+// Parts of a sequence where they have to fit.
+__host__ __device__ __forceinline__ int fitted_parts(int steps, int per) { return (steps + per - 1) / per; }
+
+// Steps of a part where the parts have to fit: from the total over the room upwards, a 32nd
+// more at a time, until no more parts are left over than there is room for (or none is cut).
+__device__ __forceinline__ int fitted_steps(const Attention &a, const Lane &first, int64_t total)
+{
+    const int longest = (a.max_kv - 1) / kStep + 1;
+    const int64_t least = total / a.fit;
+    int per = least < longest ? (int)least : longest;
+    per = per > a.min_steps ? per : a.min_steps;
+    for (;;) {
+        int64_t blocks = wave_total((int64_t)fitted_parts(first.steps, per) * first.rbs);
+        for (int b0 = 64; b0 < a.n_seqs; b0 += 64) {
+            const Lane x = lane_sequence(a, b0);
+            blocks += wave_total((int64_t)fitted_parts(x.steps, per) * x.rbs);
+        }
+        if (blocks <= a.fit || per >= longest) return per;
+        per += (per >> 5) + 1;
+    }
+}
+
 // first: the first 64 sequences.
 __device__ __forceinline__ int part_steps(const Attention &a, const Lane &first)
 {
@@ -85,7 +107,7 @@ __device__ __forceinline__ int part_steps(const Attention &a, const Lane &first)
         const Lane x = lane_sequence(a, b0);
         total += wave_total((int64_t)x.steps * x.rbs);
     }
-    return part_size(a, total);
+    return a.fit ? fitted_steps(a, first, total) : part_size(a, total);
 }
 
 // Parts of a sequence: the nearest whole number (always rounding up would cut 880 row
@@ -94,6 +116,10 @@ __host__ __device__ __forceinline__ int parts_of(int steps, int per)
 {
     const int n = (int)((steps + (per >> 1)) / per);
     return n > 0 ? n : steps > 0;
+}
+__host__ __device__ __forceinline__ int parts_of(const Attention &a, int steps, int per)
+{
+    return a.fit ? fitted_parts(steps, per) : parts_of(steps, per);
 }
 
 // Whether the items of a sequence, which begin at item `base`, are all among the planned

@@ -346,40 +346,41 @@ __global__ __launch_bounds__(256, RT > 2 ? 1 : 2) void prompt_kernel(Prompt p)
     k.run(lds);
 }
 
-// Joins the parts of a block's queries: NOPE / 4 lanes each, in the order of the parts.
+// Joins the parts of 8 or 16 queries of a block: NOPE / 4 lanes each, in the order of the parts.
 template <int MT, int NOPE>
 __global__ __launch_bounds__(256) void join_kernel(Prompt p)
 {
-    constexpr int Lanes = NOPE / 4;
-    const int item = block_of_grid() / p.q_heads, h = block_of_grid() - item * p.q_heads;
+    constexpr int Lanes = NOPE / 4, Rows = 256 / Lanes;
+    const int per = p.block_rows / Rows;   // blocks of each block of queries
+    const int at = block_of_grid() / per, piece = block_of_grid() - at * per;
+    const int item = at / p.q_heads, h = at - item * p.q_heads;
     if (item >= p.max_items) return;   // beyond the last block
     const Item x = find_item(p, item);
     if (x.b < 0) return;
+    const int row = piece * Rows + threadIdx.x / Lanes, d = 4 * (threadIdx.x & (Lanes - 1));
     const int r0 = x.rb * p.block_rows;
+    if (r0 + row >= x.nq) return;
     const int64_t next = (int64_t)p.max_items * p.q_heads * p.block_rows;   // cells from part to part
-    for (int i = threadIdx.x; i < p.block_rows * Lanes; i += 256) {
-        const int row = i / Lanes, d = 4 * (i - row * Lanes);
-        if (r0 + row >= x.nq) return;
-        const int64_t cell = ((int64_t)item * p.q_heads + h) * p.block_rows + row;
-        float top = kLowest;
-        for (int k = 0; k < p.parts; ++k) top = fmaxf(top, p.part_ml[cell + k * next].x);
-        f32x4 acc = {0, 0, 0, 0};
-        float sum = 0.0f, norm = 0.0f;
-        for (int k = 0; k < p.parts; ++k) {
-            const float4 ml = p.part_ml[cell + k * next];
-            const float f = __builtin_amdgcn_exp2f(ml.x - top);
-            sum += f * ml.y;
-            norm += f * ml.z;
-            acc += f * *reinterpret_cast<const f32x4 *>(p.part_o + (cell + k * next) * NOPE + d);
-        }
-        const float inv = norm == 0.0f ? 0.0f : 1.0f / norm;
-        const int64_t q = x.q0 + r0 + row;
-        char *to = p.out.p + (q * p.out.token_stride + (int64_t)h * p.out.head_stride + d) * 2;
-        *reinterpret_cast<u32x2 *>(to) = u32x2{pack16<MT>(acc[0] * inv, acc[1] * inv),
-                                               pack16<MT>(acc[2] * inv, acc[3] * inv)};
-        if (d == 0 && p.lse)
-            p.lse[q * p.q_heads + h] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    const int64_t cell = ((int64_t)item * p.q_heads + h) * p.block_rows + row;
+    float top = kLowest;
+    for (int k = 0; k < p.parts; ++k) top = fmaxf(top, p.part_ml[cell + k * next].x);
+    f32x4 acc = {0, 0, 0, 0};
+    float sum = 0.0f, norm = 0.0f;
+#pragma unroll 4
+    for (int k = 0; k < p.parts; ++k) {
+        const float4 ml = p.part_ml[cell + k * next];
+        const float f = __builtin_amdgcn_exp2f(ml.x - top);
+        sum += f * ml.y;
+        norm += f * ml.z;
+        acc += f * *reinterpret_cast<const f32x4 *>(p.part_o + (cell + k * next) * NOPE + d);
     }
+    const float inv = norm == 0.0f ? 0.0f : 1.0f / norm;
+    const int64_t q = x.q0 + r0 + row;
+    char *to = p.out.p + (q * p.out.token_stride + (int64_t)h * p.out.head_stride + d) * 2;
+    *reinterpret_cast<u32x2 *>(to) = u32x2{pack16<MT>(acc[0] * inv, acc[1] * inv),
+                                           pack16<MT>(acc[2] * inv, acc[3] * inv)};
+    if (d == 0 && p.lse)
+        p.lse[q * p.q_heads + h] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 template <int MT, int NOPE, int ROT, int RT>
@@ -390,7 +391,7 @@ hipError_t launch_rows(const Prompt &p, hipStream_t stream)
     prompt_kernel<MT, NOPE, ROT, RT><<<grid_of(blocks * p.parts), 256, 0, stream>>>(p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts == 1) return e;
-    join_kernel<MT, NOPE><<<grid_of(blocks), 256, 0, stream>>>(p);
+    join_kernel<MT, NOPE><<<grid_of(blocks * (p.block_rows / (1024 / NOPE))), 256, 0, stream>>>(p);
     return hipGetLastError();
 }
 

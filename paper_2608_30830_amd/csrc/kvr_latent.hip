@@ -15,7 +15,7 @@ size_t plan_latent_attention(LatentAttention &l)
     const int64_t longest = cdiv(a.max_kv, kStep);
     // Registers hold 64 rows of 512 elements a block, or 128 of 256.
     a.block_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || l.c.rank == 512 ? 64 : 128;
-    a.min_steps = 8;
+    a.min_steps = rows <= 16 ? 4 : 8;
     const int64_t blocks = std::min<int64_t>((int64_t)a.n_seqs * cdiv(rows, a.block_rows),
                                              a.n_queries * a.group / a.block_rows + a.n_seqs);
     a.target = kSlots;

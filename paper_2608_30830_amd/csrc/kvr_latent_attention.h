@@ -162,7 +162,6 @@ struct LatentTile {
         q0 = uniform(p.q0);
         rows = uniform(p.nq * a.group);
         pages = a.pages + (int64_t)uniform(p.b) * a.pages_stride;
-        hold(p.first * kStep >> a.c.page_shift);
     }
 
     // ---- rows into LDS ---------------------------------------------------------------------
@@ -447,13 +446,15 @@ struct LatentTile {
     {
         const int i0 = query_of(row), head = min(row, rows - 1) - i0 * a.group;
         const char *src = a.q.p + ((int64_t)(q0 + i0) * a.q.token_stride + (int64_t)head * a.q.head_stride) * 2;
-        const uint32_t flip = a.negate ? 0x80008000u : 0u;
         static_for<0, NB>([&](auto I) {
             constexpr int i = decltype(I)::value;
             q[i] = *reinterpret_cast<const u32x4 *>(src + (i * 32 + g * 8) * 2);
         });
         __builtin_amdgcn_sched_barrier(0);   // all loads first
-        if (flip) static_for<0, NB>([&](auto I) { q[decltype(I)::value] ^= flip; });
+    }
+    __device__ __forceinline__ static void negate(u32x4 (&q)[NB])
+    {
+        static_for<0, NB>([&](auto I) { q[decltype(I)::value] ^= 0x80008000u; });
     }
 
     // ---- results --------------------------------------------------------------------------------
@@ -636,12 +637,14 @@ struct FewRows : LatentTile<FMT, RK, RO, 32, 1> {
         char *tile = lds + wave * T::Tile;
         const uint32_t tile_at = lds_address(tile);
         int s = p.first + wave;
+        T::load_query(r0 + n, q);
+        T::hold(p.first * kStep >> a.c.page_shift);
         typename T::Codes c;
         if (s < p.last) {
             if constexpr (T::Quant) T::fetch_codes(T::locate(s * kStep, len, 0), 0, c);
             else T::fetch(T::locate(s * kStep, len, 0), 0, tile_at);
         }
-        T::load_query(r0 + n, q);
+        if (a.negate) T::negate(q);
         m = kLowest, l = 0.0f, w = 0.0f;
         static_for<0, 2 * RK>([&](auto E) { o[decltype(E)::value] = f32x4{0, 0, 0, 0}; });
         bool odd = false;
@@ -830,13 +833,15 @@ struct ManyRows : LatentTile<FMT, RK, RO, 64, WAVES> {
         const int first = p.first * kStep, end = min(len, p.last * kStep);
         const int steps = (end - first + 63) / 64;
         const uint32_t lds_at = lds_address(lds);
+        static_for<0, RT>([&](auto R) { T::load_query(row0 + 16 * decltype(R)::value + n, q[decltype(R)::value]); });
+        T::hold(p.first * kStep >> a.c.page_shift);
         typename T::Codes c;
         if constexpr (T::Quant) T::fetch_codes(T::locate(first, end, wave), wave, c);
         else T::fetch(T::locate(first, end, wave), wave, lds_at);
         if (threadIdx.x < 2) reinterpret_cast<uint32_t *>(lds + FlagAt)[threadIdx.x] = 0;
         static_for<0, RT>([&](auto R) {
             constexpr int r = decltype(R)::value;
-            T::load_query(row0 + 16 * r + n, q[r]);
+            if (a.negate) T::negate(q[r]);
             m[r] = kLowest, l[r] = 0.0f, w[r] = 0.0f;
             static_for<0, VT>([&](auto E) { o[r][decltype(E)::value] = f32x4{0, 0, 0, 0}; });
         });

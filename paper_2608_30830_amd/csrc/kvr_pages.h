@@ -10,14 +10,22 @@
 namespace kvr {
 namespace pages {
 
-constexpr int kChunkWords = 128;                // words of 64 pages that one block counts
-constexpr int kChunk = 64 * kChunkWords;        // pages
+// Free pages are the bits of words of 64.  A block counts `words` of them, a chunk: 8 to
+// 65,536, so that the chunks are at most 2,048 (each block adds up all counts).
+inline int chunk_words(int64_t n_pages)
+{
+    int words = 8;
+    while (kv::cdiv(n_pages, 64 * (int64_t)words) > 2048) words *= 2;
+    return words;
+}
+// Pools that one block goes through in one launch.
+constexpr int kSmallPages = 16384, kSmallSeqs = 1024, kSmallEntries = 65536;
 
 struct Pool {
     int32_t *refs, *table, *len;
     int64_t n_pages, stride;
     int32_t width, n_seqs, shift;               // entries of a row; log2 of the page size
-    int32_t chunks;                             // of kChunk pages
+    int32_t words, chunks;                      // words of a chunk
     int *status;
 };
 
@@ -34,7 +42,7 @@ struct Resize {
     Pool p;
     const int32_t *new_len;
     int32_t *copies;
-    uint64_t *free;     // [chunks * kChunkWords] bits of the pages that are free
+    uint64_t *free;     // [chunks * words] bits of the pages that are free
     int32_t *count;     // [chunks] of them
     Row *rows;          // [n_seqs]
 };

@@ -92,22 +92,27 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(Pool p, const int32_t *p
 
 // ---- free pages -----------------------------------------------------------------------
 
-// The free pages of chunk c as bits, and their number.
-__device__ __forceinline__ void count_chunk(const Pool &p, int c, uint64_t *free, int32_t *count,
-                                            int64_t *lds)
+// The free pages of `words` words from the block's first one on as bits, and their number.
+template <int Waves>
+__device__ __forceinline__ int count_words(const Pool &p, int64_t first, int words, uint64_t *free)
 {
-    constexpr int Words = kChunkWords / kWaves;   // of a wave
-    const int lane = threadIdx.x & 63, word = (threadIdx.x >> 6) * Words;
+    const int lane = threadIdx.x & 63;
     int sum = 0;
-#pragma unroll 8
-    for (int i = 0; i < Words; ++i) {
-        const int64_t page = (int64_t)c * kChunk + (word + i) * 64 + lane;
-        const uint64_t bits = __ballot(page < p.n_pages && p.refs[page < p.n_pages ? page : 0] <= 0);
-        if (lane == 0) free[(int64_t)c * kChunkWords + word + i] = bits;
-        sum += __popcll(bits);
+    for (int w = threadIdx.x >> 6; w < words; w += 4 * Waves) {
+        int refs[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {   // loads first
+            const int64_t page = (first + w + i * Waves) * 64 + lane;
+            refs[i] = w + i * Waves < words && page < p.n_pages ? p.refs[page] : 1;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint64_t bits = __ballot(refs[i] <= 0);
+            if (lane == 0 && w + i * Waves < words) free[w + i * Waves] = bits;
+            sum += __popcll(bits);
+        }
     }
-    const int64_t total = block_total(lane == 0 ? sum : 0, lds);
-    if (threadIdx.x == 0) count[c] = (int)total;
+    return lane == 0 ? sum : 0;
 }
 
 // Free pages before chunk c, and of all chunks.
@@ -124,25 +129,22 @@ __device__ __forceinline__ void free_before(const int32_t *count, int chunks, in
     all = block_total(y, lds);
 }
 
-// Calls f(page, free, its rank among the free) for the pages of chunk c, of which `before` free
-// ones come before.
-template <class F>
-__device__ __forceinline__ void rank_chunk(const uint64_t *free, int c, int64_t before, int64_t n_pages, F f)
+// The pages of `words` words from the block's first one on, of which `before` free ones come
+// before: f(page, free, rank among the free).  Each wave counts the words before its own.
+template <int Waves, class F>
+__device__ __forceinline__ void rank_words(const Pool &p, const uint64_t *free, int64_t first, int words,
+                                           int64_t before, F f)
 {
-    constexpr int Words = kChunkWords / kWaves;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // words of the chunk two a lane: their bits before each
-    const uint64_t *w = free + (int64_t)c * kChunkWords;
-    const int a = __popcll(w[2 * lane]), b = __popcll(w[2 * lane + 1]);
-    const int upto = wave_incl_scan(a + b);
-    for (int i = 0; i < Words; ++i) {
-        const int word = wave * Words + i, l = word >> 1;
-        const int first = __builtin_amdgcn_readlane(upto - (a + b), l) +
-                          ((word & 1) ? __builtin_amdgcn_readlane(a, l) : 0);
-        const uint64_t bits = w[word];
-        const int64_t page = (int64_t)c * kChunk + word * 64 + lane;
-        if (page < n_pages)
-            f(page, (bits >> lane & 1) != 0, before + first + __popcll(bits & ((1ull << lane) - 1)));
+    const int per = (words + Waves - 1) / Waves, w0 = wave * per, w1 = min(w0 + per, words);
+    int64_t x = 0;
+    for (int w = lane; w < w0; w += 64) x += __popcll(free[w]);
+    int64_t rank = before + wave_total(x);
+    for (int w = w0; w < w1; ++w) {
+        const uint64_t bits = free[w];
+        const int64_t page = (first + w) * 64 + lane;
+        if (page < p.n_pages) f(page, (bits >> lane & 1) != 0, rank + __popcll(bits & ((1ull << lane) - 1)));
+        rank += __popcll(bits);
     }
 }
 
@@ -150,13 +152,98 @@ __device__ __forceinline__ void rank_chunk(const uint64_t *free, int c, int64_t 
 
 enum { kLeave = 0, kBack = 1, kGrow = 2, kGrowOwn = 3, kBad = 4 };
 
-// The last block plans the rows, the others count free pages.
+// What row b does, but for its start.
+__device__ __forceinline__ Row plan_row(const Resize &r, int b)
+{
+    const Pool &p = r.p;
+    Row x{};
+    const int want = r.new_len[b], len = p.len[b];
+    if (want < 0) return x;
+    const int have = entries(p, len), need = entries(p, want);
+    x.need = need;
+    x.first = have;
+    if (have < 0 || need < 0) {
+        x.mode = kBad;
+    } else if (want <= len) {
+        x.mode = want < len ? kBack : kLeave;
+    } else {
+        x.mode = kGrow;
+        x.take = need - have;
+        if (len & ((1 << p.shift) - 1)) {   // into a page that others hold too?
+            const int last = p.table[(int64_t)b * p.stride + have - 1];
+            if (!in_pool(p, last)) {
+                x.mode = kBad;
+                x.take = 0;
+            } else if (p.refs[last] > 1) {
+                x.mode = kGrowOwn;
+                x.take += 1;
+                x.first -= 1;
+            }
+        }
+    }
+    return x;
+}
+
+// Page `page`, free and of this rank, goes to row b.
+__device__ __forceinline__ void give(const Resize &r, int b, const Row &x, int64_t page, int64_t rank)
+{
+    const Pool &p = r.p;
+    int32_t *entry = p.table + (int64_t)b * p.stride + x.first + (rank - x.start);
+    if (x.mode == kGrowOwn && rank == x.start) {
+        const int old = *entry;
+        r.copies[2 * (int64_t)b] = old;
+        r.copies[2 * (int64_t)b + 1] = (int)page;
+        give_back(p, old);
+    }
+    *entry = (int)page;
+    p.refs[page] = 1;
+}
+
+// Row b's length, and its pages to copy if there are none; all: the pages that are free.
+__device__ __forceinline__ void end_row(const Resize &r, int b, const Row &x, int64_t all)
+{
+    const bool grows = (x.mode == kGrow || x.mode == kGrowOwn) && (x.take == 0 || x.start + x.take <= all);
+    if (x.mode == kBad || (x.mode >= kGrow && !grows)) report(r.p);
+    if (!(grows && x.mode == kGrowOwn)) r.copies[2 * (int64_t)b] = r.copies[2 * (int64_t)b + 1] = -1;
+    if (grows || x.mode == kBack) r.p.len[b] = r.new_len[b];
+}
+// The rest of what row b does, by one wave.
+__device__ __forceinline__ void finish_row(const Resize &r, int b, const Row &x, int64_t all)
+{
+    const Pool &p = r.p;
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) end_row(r, b, x, all);
+    if (x.mode == kBack) {
+        int32_t *row = p.table + (int64_t)b * p.stride;
+        for (int i = x.need + lane; i < x.first; i += 64) {
+            give_back(p, row[i]);
+            row[i] = -1;
+        }
+    }
+}
+
+// The last row that starts at or before a rank.
+template <class Start>
+__device__ __forceinline__ int row_of_rank(int n_seqs, int64_t rank, Start start)
+{
+    int lo = 0, hi = n_seqs;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start(mid) <= rank) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// The first block plans the rows, the others count free pages.
 __global__ __launch_bounds__(kThreads) void resize_plan_kernel(Resize r)
 {
     __shared__ int64_t lds[kWaves];
     const Pool &p = r.p;
     if ((int)blockIdx.x > 0) {
-        count_chunk(p, blockIdx.x - 1, r.free, r.count, lds);
+        const int c = blockIdx.x - 1;
+        const int64_t n = block_total(count_words<kWaves>(p, (int64_t)c * p.words, p.words, r.free + (int64_t)c * p.words), lds);
+        if (threadIdx.x == 0) r.count[c] = (int)n;
         return;
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -164,34 +251,7 @@ __global__ __launch_bounds__(kThreads) void resize_plan_kernel(Resize r)
     for (int b0 = 0; b0 < p.n_seqs; b0 += kThreads) {
         const int b = b0 + threadIdx.x;
         Row x{};
-        if (b < p.n_seqs) {
-            const int want = r.new_len[b];
-            if (want >= 0) {
-                const int len = p.len[b];
-                const int have = entries(p, len), need = entries(p, want);
-                x.need = need;
-                x.first = have;
-                if (have < 0 || need < 0) {
-                    x.mode = kBad;
-                } else if (want <= len) {
-                    x.mode = want < len ? kBack : kLeave;
-                } else {
-                    x.mode = kGrow;
-                    x.take = need - have;
-                    if (len & ((1 << p.shift) - 1)) {   // into a page that others hold too?
-                        const int last = p.table[(int64_t)b * p.stride + have - 1];
-                        if (!in_pool(p, last)) {
-                            x.mode = kBad;
-                            x.take = 0;
-                        } else if (p.refs[last] > 1) {
-                            x.mode = kGrowOwn;
-                            x.take += 1;
-                            x.first -= 1;
-                        }
-                    }
-                }
-            }
-        }
+        if (b < p.n_seqs) x = plan_row(r, b);
         const int64_t upto = wave_incl_scan((int64_t)x.take);
         if (lane == 63) lds[wave] = upto;
         __syncthreads();
@@ -219,105 +279,131 @@ __global__ __launch_bounds__(kThreads) void resize_apply_kernel(Resize r)
         const Row tail = r.rows[p.n_seqs - 1];
         const int64_t taken = tail.start + tail.take;
         if (before >= taken) return;
-        rank_chunk(r.free, c, before, p.n_pages, [&](int64_t page, bool free, int64_t rank) {
+        rank_words<kWaves>(p, r.free + (int64_t)c * p.words, (int64_t)c * p.words, p.words, before,
+                           [&](int64_t page, bool free, int64_t rank) {
             if (!free || rank >= taken) return;
-            int lo = 0, hi = p.n_seqs;   // the last row that starts at or before the rank
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (r.rows[mid].start <= rank) lo = mid;
-                else hi = mid;
-            }
-            const Row x = r.rows[lo];
-            if (x.start + x.take > all) return;   // it does not fit
-            int32_t *entry = p.table + (int64_t)lo * p.stride + x.first + (rank - x.start);
-            if (x.mode == kGrowOwn && rank == x.start) {
-                const int old = *entry;
-                r.copies[2 * (int64_t)lo] = old;
-                r.copies[2 * (int64_t)lo + 1] = (int)page;
-                give_back(p, old);
-            }
-            *entry = (int)page;
-            p.refs[page] = 1;
+            const int b = row_of_rank(p.n_seqs, rank, [&](int i) { return r.rows[i].start; });
+            const Row x = r.rows[b];
+            if (x.start + x.take <= all) give(r, b, x, page, rank);
         });
         return;
     }
-    const int b = (c - p.chunks) * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (b >= p.n_seqs) return;
-    const Row x = r.rows[b];
-    const bool grows = (x.mode == kGrow || x.mode == kGrowOwn) && (x.take == 0 || x.start + x.take <= all);
-    if (x.mode == kBad || (x.mode >= kGrow && !grows)) report(p);
-    if (lane == 0) {
-        if (!(grows && x.mode == kGrowOwn)) r.copies[2 * (int64_t)b] = r.copies[2 * (int64_t)b + 1] = -1;
-        if (grows || x.mode == kBack) p.len[b] = r.new_len[b];
+    const int b = (c - p.chunks) * kWaves + (threadIdx.x >> 6);
+    if (b < p.n_seqs) finish_row(r, b, r.rows[b], all);
+}
+
+// The same for a small pool, by one block, rows in LDS.  (The counts of free pages are taken before
+// any changes.)  What rows give back is spread over all threads, four entries each at a time: the
+// atomics of one wait together.
+constexpr int kWide = 1024, kWideWaves = kWide / 64;
+
+// Exclusive sum over the block's threads; total: of all.  lds: [kWideWaves].
+__device__ __forceinline__ int64_t wide_scan(int64_t x, int64_t *lds, int64_t &total)
+{
+    const int64_t upto = wave_incl_scan(x);
+    if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = upto;
+    __syncthreads();
+    int64_t before = upto - x;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kWideWaves; ++w) {
+        if (w < (int)(threadIdx.x >> 6)) before += lds[w];
+        total += lds[w];
     }
-    if (x.mode == kBack) {
-        int32_t *row = p.table + (int64_t)b * p.stride;
-        for (int i = x.need + lane; i < x.first; i += 64) {
-            give_back(p, row[i]);
-            row[i] = -1;
+    __syncthreads();
+    return before;
+}
+
+__global__ __launch_bounds__(kWide) void resize_small_kernel(Resize r)
+{
+    __shared__ uint64_t free[kSmallPages / 64];
+    __shared__ Row rows[kSmallSeqs];
+    __shared__ int32_t back[kSmallSeqs];   // entries that the rows before give back
+    __shared__ int64_t sums[kWideWaves];
+    const Pool &p = r.p;
+    const int lane = threadIdx.x & 63;
+    const int words = (int)((p.n_pages + 63) >> 6);
+    const int mine = wave_total(count_words<kWideWaves>(p, 0, words, free));
+    const int b = threadIdx.x;   // at most kWide rows
+    Row x{};
+    if (b < p.n_seqs) x = plan_row(r, b);
+    int64_t all, taken, returned;
+    wide_scan(lane == 0 ? mine : 0, sums, all);
+    x.start = wide_scan(x.take, sums, taken);
+    back[b] = (int32_t)wide_scan(x.mode == kBack ? x.first - x.need : 0, sums, returned);
+    rows[b] = x;
+    __syncthreads();
+    rank_words<kWideWaves>(p, free, 0, words, 0, [&](int64_t page, bool is_free, int64_t rank) {
+        if (!is_free || rank >= taken) return;
+        const int to = row_of_rank(p.n_seqs, rank, [&](int i) { return rows[i].start; });
+        const Row y = rows[to];
+        if (y.start + y.take <= all) give(r, to, y, page, rank);
+    });
+    for (int i0 = threadIdx.x; i0 < returned; i0 += 4 * kWide) {
+        int32_t *at[4];
+        int page[4], held[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = i0 + k * kWide;
+            at[k] = nullptr;
+            if (i >= returned) continue;
+            const int of = row_of_rank(p.n_seqs, i, [&](int j) { return (int64_t)back[j]; });
+            at[k] = p.table + (int64_t)of * p.stride + rows[of].need + (i - back[of]);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) page[k] = at[k] ? *at[k] : 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) held[k] = at[k] && in_pool(p, page[k]) ? atomicSub(p.refs + page[k], 1) : 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (!at[k]) continue;
+            if (held[k] <= 0) {   // outside the pool, or given back more often than held
+                if (in_pool(p, page[k])) atomicAdd(p.refs + page[k], 1);
+                report(p);
+            }
+            *at[k] = -1;
         }
     }
+    if (b < p.n_seqs) end_row(r, b, x, all);
 }
 
 // ---- compaction -----------------------------------------------------------------------
 
-__global__ __launch_bounds__(kThreads) void count_kernel(Compact c)
-{
-    __shared__ int64_t lds[kWaves];
-    count_chunk(c.p, blockIdx.x, c.free, c.count, lds);
-}
-
 // With U pages in use, the k-th lowest hole below U takes the k-th highest page in use, which
 // lies at or beyond U: there are as many of one as of the other.
-__global__ __launch_bounds__(kThreads) void pair_kernel(Compact c)
+__device__ __forceinline__ void pair_page(const Compact &c, int64_t page, bool free, int64_t rank, int64_t used,
+                                          int64_t limit)
 {
-    __shared__ int64_t lds[kWaves];
-    const Pool &p = c.p;
-    int64_t before, all, holes, same;
-    free_before(c.count, p.chunks, blockIdx.x, before, all, lds);
-    const int64_t used = p.n_pages - all;
-    // holes below U: in whole chunks, and in the words of U's own
-    free_before(c.count, p.chunks, (int)(used / kChunk), holes, same, lds);
-    if (used < p.n_pages) {
-        const int64_t first = used / kChunk * kChunkWords, last = used / 64;   // words
-        int64_t n = 0;
-        for (int64_t w = first + threadIdx.x; w <= last; w += kThreads) {
-            const uint64_t bits = c.free[w];
-            n += __popcll(w < last ? bits : bits & ((1ull << (used & 63)) - 1));
-        }
-        holes += block_total(n, lds);
-    }
-    const int64_t limit = min(holes, c.max_moves);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *c.used = (int)used;
-    rank_chunk(c.free, blockIdx.x, before, p.n_pages, [&](int64_t page, bool free, int64_t rank) {
-        if (page >= limit && page < c.max_moves) c.moves[2 * page] = c.moves[2 * page + 1] = -1;
-        if (page < used) {
-            if (free && rank < limit) c.moves[2 * rank + 1] = (int)page;
-            return;
-        }
-        const int64_t k = used - 1 - (page - rank);   // among those in use, from the highest
-        const bool moves = !free && k < limit;
-        if (moves) c.moves[2 * k] = (int)page;
-        c.where[page] = moves ? (int)k : -1;
-    });
-}
-
-// The first blocks carry the counts over, the others change four rows of the table each.
-__global__ __launch_bounds__(kThreads) void move_kernel(Compact c, int move_blocks)
-{
-    const Pool &p = c.p;
-    if ((int)blockIdx.x < move_blocks) {
-        const int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-        if (k >= c.max_moves) return;
-        const int from = c.moves[2 * k], to = c.moves[2 * k + 1];
-        if (from < 0) return;
-        p.refs[to] = p.refs[from];
-        p.refs[from] = 0;
+    if (page >= limit && page < c.max_moves) c.moves[2 * page] = c.moves[2 * page + 1] = -1;
+    if (page < used) {
+        if (free && rank < limit) c.moves[2 * rank + 1] = (int)page;
         return;
     }
-    const int b = (blockIdx.x - move_blocks) * kWaves + (threadIdx.x >> 6);
-    if (b >= p.n_seqs) return;
-    const int n = entries(p, p.len[b]), used = *c.used;
+    const int64_t k = used - 1 - (page - rank);   // among those in use, from the highest
+    const bool moves = !free && k < limit;
+    if (moves) c.moves[2 * k] = (int)page;
+    c.where[page] = moves ? (int)k : -1;
+}
+// Free pages before `used` among words from `first` on that begin before it.
+__device__ __forceinline__ int64_t holes_of(const uint64_t *free, int64_t first, int64_t used, int threads)
+{
+    int64_t n = 0;
+    for (int64_t w = first + threadIdx.x; w * 64 < used; w += threads)
+        n += __popcll((w + 1) * 64 <= used ? free[w] : free[w] & ((1ull << (used & 63)) - 1));
+    return n;
+}
+__device__ __forceinline__ void move_counts(const Compact &c, int64_t k)
+{
+    const int from = c.moves[2 * k], to = c.moves[2 * k + 1];
+    if (from < 0) return;
+    c.p.refs[to] = c.p.refs[from];
+    c.p.refs[from] = 0;
+}
+// One wave changes row b of the table.
+__device__ __forceinline__ void move_row(const Compact &c, int b, int used)
+{
+    const Pool &p = c.p;
+    const int n = entries(p, p.len[b]);
     if (n < 0) report(p);
     int32_t *row = p.table + (int64_t)b * p.stride;
     for (int i = threadIdx.x & 63; i < n; i += 64) {
@@ -329,6 +415,71 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Compact c, int move_bloc
             if (k >= 0) row[i] = c.moves[2 * (int64_t)k + 1];
         }
     }
+}
+
+__global__ __launch_bounds__(kThreads) void count_kernel(Compact c)
+{
+    __shared__ int64_t lds[kWaves];
+    const int64_t first = (int64_t)blockIdx.x * c.p.words;
+    const int64_t n = block_total(count_words<kWaves>(c.p, first, c.p.words, c.free + first), lds);
+    if (threadIdx.x == 0) c.count[blockIdx.x] = (int)n;
+}
+
+__global__ __launch_bounds__(kThreads) void pair_kernel(Compact c)
+{
+    __shared__ int64_t lds[kWaves];
+    const Pool &p = c.p;
+    int64_t before, all, holes, same;
+    free_before(c.count, p.chunks, blockIdx.x, before, all, lds);
+    const int64_t used = p.n_pages - all, chunk = used / (64 * (int64_t)p.words);
+    // holes below U: in whole chunks, and in the words of U's own
+    free_before(c.count, p.chunks, (int)chunk, holes, same, lds);
+    holes += block_total(holes_of(c.free, chunk * p.words, used, kThreads), lds);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *c.used = (int)used;
+    const int64_t first = (int64_t)blockIdx.x * p.words, limit = min(holes, c.max_moves);
+    rank_words<kWaves>(p, c.free + first, first, p.words, before,
+                       [&](int64_t page, bool free, int64_t rank) { pair_page(c, page, free, rank, used, limit); });
+}
+
+// The first blocks carry the counts over, the others change four rows of the table each.
+__global__ __launch_bounds__(kThreads) void move_kernel(Compact c, int move_blocks)
+{
+    if ((int)blockIdx.x < move_blocks) {
+        const int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+        if (k < c.max_moves) move_counts(c, k);
+        return;
+    }
+    const int b = (blockIdx.x - move_blocks) * kWaves + (threadIdx.x >> 6);
+    if (b < c.p.n_seqs) move_row(c, b, *c.used);
+}
+
+// The same for a small pool, by one block.
+__global__ __launch_bounds__(kWide) void compact_small_kernel(Compact c)
+{
+    __shared__ uint64_t free[kSmallPages / 64];
+    __shared__ int part[kWideWaves], hole[kWideWaves];
+    const Pool &p = c.p;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int words = (int)((p.n_pages + 63) >> 6);
+    const int mine = wave_total(count_words<kWideWaves>(p, 0, words, free));
+    if (lane == 0) part[wave] = mine;
+    __syncthreads();
+    int64_t used = p.n_pages;
+#pragma unroll
+    for (int w = 0; w < kWideWaves; ++w) used -= part[w];
+    const int64_t holes = wave_total(holes_of(free, 0, used, kWide));
+    if (lane == 0) hole[wave] = (int)holes;
+    __syncthreads();
+    int64_t limit = 0;
+#pragma unroll
+    for (int w = 0; w < kWideWaves; ++w) limit += hole[w];
+    limit = min(limit, c.max_moves);
+    if (threadIdx.x == 0) *c.used = (int)used;
+    rank_words<kWideWaves>(p, free, 0, words, 0,
+                           [&](int64_t page, bool is_free, int64_t rank) { pair_page(c, page, is_free, rank, used, limit); });
+    __syncthreads();   // moves and `where` are complete
+    for (int64_t k = threadIdx.x; k < limit; k += kWide) move_counts(c, k);
+    for (int b = wave; b < p.n_seqs; b += kWideWaves) move_row(c, b, (int)used);
 }
 
 // ---- copies ---------------------------------------------------------------------------
@@ -389,6 +540,11 @@ hipError_t launch_fork(const Pool &p, const int32_t *parent, hipStream_t stream)
 
 hipError_t launch_resize(const Resize &r, hipStream_t stream)
 {
+    if (r.p.n_pages <= kSmallPages && r.p.n_seqs <= kSmallSeqs &&
+        (int64_t)r.p.n_seqs * r.p.width <= kSmallEntries) {
+        resize_small_kernel<<<1, kWide, 0, stream>>>(r);
+        return hipGetLastError();
+    }
     resize_plan_kernel<<<r.p.chunks + 1, kThreads, 0, stream>>>(r);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -398,6 +554,10 @@ hipError_t launch_resize(const Resize &r, hipStream_t stream)
 
 hipError_t launch_compact(const Compact &c, hipStream_t stream)
 {
+    if (c.p.n_pages <= kSmallPages && (int64_t)c.p.n_seqs * c.p.width <= kSmallEntries) {
+        compact_small_kernel<<<1, kWide, 0, stream>>>(c);
+        return hipGetLastError();
+    }
     count_kernel<<<c.p.chunks, kThreads, 0, stream>>>(c);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -10,8 +10,6 @@ namespace {
 
 using kvr::pages::Compact;
 using kvr::pages::Copy;
-using kvr::pages::kChunk;
-using kvr::pages::kChunkWords;
 using kvr::pages::Pool;
 using kvr::pages::Resize;
 
@@ -34,7 +32,8 @@ int check_pool(const kvr_page_pool *p, int32_t *status, Pool &out)
     out.width = p->max_pages;
     out.n_seqs = p->n_seqs;
     out.shift = __builtin_ctz((unsigned)ps);
-    out.chunks = (int32_t)kvr::kv::cdiv(p->n_pages, kChunk);
+    out.words = kvr::pages::chunk_words(p->n_pages);
+    out.chunks = (int32_t)kvr::kv::cdiv(p->n_pages, 64 * (int64_t)out.words);
     out.status = status;
     return KVR_OK;
 }
@@ -95,7 +94,7 @@ int kvr_pages_resize(const kvr_page_pool *pool, const int32_t *d_new_len, int32_
     int rc = check_pool(pool, d_status, r.p);
     if (rc != KVR_OK) return rc;
     if (!ws_bytes) return KVR_E_NULL;
-    const size_t free = (size_t)r.p.chunks * kChunkWords * sizeof(uint64_t);
+    const size_t free = (size_t)r.p.chunks * r.p.words * sizeof(uint64_t);
     const size_t count = round256((size_t)r.p.chunks * sizeof(int32_t));
     const size_t need = free + count + (size_t)r.p.n_seqs * sizeof(kvr::pages::Row);
     if (!d_ws) {
@@ -125,7 +124,7 @@ int kvr_pages_compact(const kvr_page_pool *pool, int32_t *d_moves, int64_t max_m
     if (rc != KVR_OK) return rc;
     if (!ws_bytes) return KVR_E_NULL;
     if (max_moves < 0 || max_moves > c.p.n_pages) return KVR_E_SIZE;
-    const size_t free = (size_t)c.p.chunks * kChunkWords * sizeof(uint64_t);
+    const size_t free = (size_t)c.p.chunks * c.p.words * sizeof(uint64_t);
     const size_t count = round256((size_t)c.p.chunks * sizeof(int32_t));
     const size_t need = free + count + (size_t)c.p.n_pages * sizeof(int32_t);
     if (!d_ws) {

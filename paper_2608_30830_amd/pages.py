@@ -60,7 +60,7 @@ class PageBuffers:
             raise ValueError("the caches of a pool must be on one device")
         tensors = [t for c in caches for t in c.tensors if t is not None]
         # tensors whose pages are alike next to each other: they are copied together
-        tensors.sort(key=lambda t: (-t.element_size() * t[0].numel(), tuple(t.stride())))
+        tensors.sort(key=lambda t: (-t.element_size() * t.shape[1:].numel(), tuple(t.stride())))
         self.caches, self.n_pages, self.device = caches, caches[0].n_pages, caches[0].device
         self.c = c = (kvr_page_buffer * len(tensors))()
         for b, t in zip(c, tensors):

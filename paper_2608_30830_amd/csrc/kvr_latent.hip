@@ -20,8 +20,9 @@ size_t plan_latent_attention(LatentAttention &l)
                                              a.n_queries * a.group / a.block_rows + a.n_seqs);
     a.target = kSlots;
     a.fit = kSlots;   // a block more than there is room for begins another round
+    // (fitted_steps cuts for several rounds only where the row blocks exceed half a round)
     a.max_items = (int32_t)std::max<int64_t>(
-        1, std::min(std::max<int64_t>(kSlots, blocks), blocks * cdiv(longest, a.min_steps)));
+        1, std::min(2 * blocks > kSlots ? blocks + 2 * kSlots : kSlots, blocks * cdiv(longest, a.min_steps)));
     a.direct = 0;
     if (longest <= a.min_steps) {
         const int64_t room = cdiv(rows, a.block_rows);

@@ -657,7 +657,7 @@ struct FewRows : LatentTile<FMT, RK, RO, 32, 1> {
             }
             odd |= compute(s, query, tile);
             if constexpr (!T::Quant) {
-                asm volatile("" ::: "memory");   // the tile has been read
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the tile has been read
                 if (s + Waves < p.last) T::fetch(T::locate((s + Waves) * kStep, len, 0), 0, tile_at);
             }
         }

@@ -47,6 +47,24 @@ __device__ __forceinline__ void give_back(const Pool &p, int page)
         report(p);
     }
 }
+// Up to four entries, which become -1: the atomics of one wait together.
+__device__ __forceinline__ void give_back(const Pool &p, int32_t *const (&at)[4])
+{
+    int page[4], held[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) page[k] = at[k] ? *at[k] : 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) held[k] = at[k] && in_pool(p, page[k]) ? atomicSub(p.refs + page[k], 1) : 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (!at[k]) continue;
+        if (held[k] <= 0) {   // outside the pool, or given back more often than held
+            if (in_pool(p, page[k])) atomicAdd(p.refs + page[k], 1);
+            report(p);
+        }
+        *at[k] = -1;
+    }
+}
 
 // Sum over a block, the same in every thread.
 __device__ __forceinline__ int64_t block_total(int64_t x, int64_t *lds)
@@ -215,9 +233,11 @@ __device__ __forceinline__ void finish_row(const Resize &r, int b, const Row &x,
     if (lane == 0) end_row(r, b, x, all);
     if (x.mode == kBack) {
         int32_t *row = p.table + (int64_t)b * p.stride;
-        for (int i = x.need + lane; i < x.first; i += 64) {
-            give_back(p, row[i]);
-            row[i] = -1;
+        for (int i = x.need + lane; i < x.first; i += 4 * 64) {
+            int32_t *at[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) at[k] = i + k * 64 < x.first ? row + i + k * 64 : nullptr;
+            give_back(p, at);
         }
     }
 }
@@ -316,7 +336,7 @@ __device__ __forceinline__ int64_t wide_scan(int64_t x, int64_t *lds, int64_t &t
 
 __global__ __launch_bounds__(kWide) void resize_small_kernel(Resize r)
 {
-    __shared__ uint64_t free[kSmallPages / 64];
+    __shared__ uint64_t free[kSmallResize / 64];
     __shared__ Row rows[kSmallSeqs];
     __shared__ int32_t back[kSmallSeqs];   // entries that the rows before give back
     __shared__ int64_t sums[kWideWaves];
@@ -341,7 +361,6 @@ __global__ __launch_bounds__(kWide) void resize_small_kernel(Resize r)
     });
     for (int i0 = threadIdx.x; i0 < returned; i0 += 4 * kWide) {
         int32_t *at[4];
-        int page[4], held[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int i = i0 + k * kWide;
@@ -350,19 +369,7 @@ __global__ __launch_bounds__(kWide) void resize_small_kernel(Resize r)
             const int of = row_of_rank(p.n_seqs, i, [&](int j) { return (int64_t)back[j]; });
             at[k] = p.table + (int64_t)of * p.stride + rows[of].need + (i - back[of]);
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) page[k] = at[k] ? *at[k] : 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) held[k] = at[k] && in_pool(p, page[k]) ? atomicSub(p.refs + page[k], 1) : 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (!at[k]) continue;
-            if (held[k] <= 0) {   // outside the pool, or given back more often than held
-                if (in_pool(p, page[k])) atomicAdd(p.refs + page[k], 1);
-                report(p);
-            }
-            *at[k] = -1;
-        }
+        give_back(p, at);
     }
     if (b < p.n_seqs) end_row(r, b, x, all);
 }
@@ -456,7 +463,7 @@ __global__ __launch_bounds__(kThreads) void move_kernel(Compact c, int move_bloc
 // The same for a small pool, by one block.
 __global__ __launch_bounds__(kWide) void compact_small_kernel(Compact c)
 {
-    __shared__ uint64_t free[kSmallPages / 64];
+    __shared__ uint64_t free[kSmallCompact / 64];
     __shared__ int part[kWideWaves], hole[kWideWaves];
     const Pool &p = c.p;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -540,8 +547,8 @@ hipError_t launch_fork(const Pool &p, const int32_t *parent, hipStream_t stream)
 
 hipError_t launch_resize(const Resize &r, hipStream_t stream)
 {
-    if (r.p.n_pages <= kSmallPages && r.p.n_seqs <= kSmallSeqs &&
-        (int64_t)r.p.n_seqs * r.p.width <= kSmallEntries) {
+    const int64_t entries = (int64_t)r.p.n_seqs * r.p.width;
+    if (r.p.n_pages <= kSmallResize && r.p.n_seqs <= kSmallSeqs && entries <= kSmallEntries) {
         resize_small_kernel<<<1, kWide, 0, stream>>>(r);
         return hipGetLastError();
     }
@@ -554,7 +561,8 @@ hipError_t launch_resize(const Resize &r, hipStream_t stream)
 
 hipError_t launch_compact(const Compact &c, hipStream_t stream)
 {
-    if (c.p.n_pages <= kSmallPages && (int64_t)c.p.n_seqs * c.p.width <= kSmallEntries) {
+    const int64_t entries = (int64_t)c.p.n_seqs * c.p.width;
+    if (c.p.n_pages <= kSmallCompact && c.p.n_seqs <= kFewSeqs && entries <= kSmallEntries) {
         compact_small_kernel<<<1, kWide, 0, stream>>>(c);
         return hipGetLastError();
     }

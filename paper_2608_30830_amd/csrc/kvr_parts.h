@@ -29,14 +29,18 @@ __device__ __forceinline__ int lane_value(int x, int lane)   // uniform
 }
 
 // Tokens, new tokens and first query of sequence b; false where they do not fit the call.
+__host__ __device__ __forceinline__ bool sequence_fits(const Attention &a, int len, int nq, int q0)
+{
+    return q0 >= 0 && nq >= 0 && nq <= a.max_q && (int64_t)q0 + nq <= a.n_queries && len >= nq &&
+           len <= a.max_kv &&
+           (((int64_t)len + (1 << a.c.page_shift) - 1) >> a.c.page_shift) <= a.max_pages;
+}
 __host__ __device__ __forceinline__ bool sequence(const Attention &a, int b, int &len, int &nq, int &q0)
 {
     q0 = a.cu_q[b];
     nq = a.cu_q[b + 1] - q0;
     len = a.kv_len[b];
-    const bool ok = q0 >= 0 && nq >= 0 && nq <= a.max_q && (int64_t)q0 + nq <= a.n_queries &&
-                    len >= nq && len <= a.max_kv &&
-                    (((int64_t)len + (1 << a.c.page_shift) - 1) >> a.c.page_shift) <= a.max_pages;
+    const bool ok = sequence_fits(a, len, nq, q0);
     if (!ok) {
         if (a.status) *a.status = KVR_E_DOMAIN;
         len = nq = 0;
@@ -77,37 +81,124 @@ __host__ __device__ __forceinline__ int part_size(const Attention &a, int64_t to
     const int per = n < (double)longest ? (int)n : longest;
     return per > a.min_steps ? per : a.min_steps;
 }
-// Parts of a sequence where they have to fit.
+// Parts of at most `per` steps of a sequence.
 __host__ __device__ __forceinline__ int fitted_parts(int steps, int per) { return (steps + per - 1) / per; }
 
-// Steps of a part where the parts have to fit: from the total over the room upwards, a 32nd
-// more at a time, until no more parts are left over than there is room for (or none is cut).
-__device__ __forceinline__ int fitted_steps(const Attention &a, const Lane &first, int64_t total)
+// Steps of a part where a part's block occupies its CU alone: a round of them is a.fit blocks, and
+// one block more begins another round.  total: all steps, of each row block; blocks: row blocks;
+// count(per): the parts of at most `per` steps, of all row blocks.
+//
+// One round: the fewest steps, to a 32nd, that leave no more parts than fit.  The parts of `per`
+// steps are fewer than total / per + blocks, which bounds the search from above.
+// Where the row blocks alone take more than half a round, parts that do fit may be as long as the
+// sequences: then parts of a half of what each of a round's blocks would get, in as many rounds as
+// that takes, if that ends sooner; each of them costs about eight steps more, for its beginning and
+// for its way through memory.
+template <class Count>
+__host__ __device__ __forceinline__ int fitted_steps(const Attention &a, int64_t total, int64_t blocks,
+                                                     Count count)
 {
     const int longest = (a.max_kv - 1) / kStep + 1;
-    const int64_t least = total / a.fit;
-    int per = least < longest ? (int)least : longest;
-    per = per > a.min_steps ? per : a.min_steps;
-    for (;;) {
-        int64_t blocks = wave_total((int64_t)fitted_parts(first.steps, per) * first.rbs);
-        for (int b0 = 64; b0 < a.n_seqs; b0 += 64) {
-            const Lane x = lane_sequence(a, b0);
-            blocks += wave_total((int64_t)fitted_parts(x.steps, per) * x.rbs);
+    auto bounded = [&](int64_t n, int least) { return n >= longest ? longest : n > least ? (int)n : least; };
+    int per = longest;
+    if (blocks < a.fit) {
+        int lo = bounded(total / a.fit, a.min_steps);
+        per = bounded(total / (a.fit - blocks) + 1, lo);
+        if (lo >= per || count(lo) <= a.fit) {
+            per = lo;
+        } else {
+            while (per - lo > 1 + (lo >> 5)) {
+                const int mid = lo + (per - lo) / 2;
+                if (count(mid) <= a.fit) per = mid;
+                else lo = mid;
+            }
         }
-        if (blocks <= a.fit || per >= longest) return per;
-        per += (per >> 5) + 1;
     }
+    if (2 * blocks <= a.fit) return per;
+    const int many = bounded(total / (2 * a.fit) + 1, 2 * a.min_steps);
+    if (many >= per) return per;
+    const int64_t rounds = blocks <= a.fit ? 1 : (blocks + a.fit - 1) / a.fit;
+    const int64_t others = (count(many) + a.fit - 1) / a.fit;
+    return others * (many + 8) < rounds * per ? many : per;
 }
+
+// 256 sequences, four a lane, their loads on the way together.  (One group of 64 after the other
+// took 20 us more in 256 blocks of 256 sequences.)
+struct Lanes {
+    static constexpr int Groups = 4, Most = 64 * Groups;
+    int steps[Groups], rbs[Groups];
+    __device__ __forceinline__ void load(const Attention &a, int b0)
+    {
+        const int lane = threadIdx.x & 63, last = a.n_seqs - 1;
+        int q0[Groups], next[Groups], len[Groups];
+#pragma unroll
+        for (int i = 0; i < Groups; ++i) {
+            const int b = min(b0 + 64 * i + lane, last);
+            q0[i] = a.cu_q[b], next[i] = a.cu_q[b + 1], len[i] = a.kv_len[b];
+        }
+#pragma unroll
+        for (int i = 0; i < Groups; ++i) {
+            const int nq = next[i] - q0[i];
+            bool ok = sequence_fits(a, len[i], nq, q0[i]);
+            if (!ok && a.status) *a.status = KVR_E_DOMAIN;
+            ok = ok && b0 + 64 * i + lane <= last;
+            steps[i] = ok ? steps_of(len[i], nq) : 0;
+            rbs[i] = ok ? row_blocks_of(a, nq) : 0;
+        }
+    }
+    // This lane's steps times row blocks, and parts.
+    __device__ __forceinline__ int64_t total() const
+    {
+        int64_t n = 0;
+#pragma unroll
+        for (int i = 0; i < Groups; ++i) n += (int64_t)steps[i] * rbs[i];
+        return n;
+    }
+    __device__ __forceinline__ int64_t parts(int per) const
+    {
+        int64_t n = 0;
+#pragma unroll
+        for (int i = 0; i < Groups; ++i) n += (int64_t)fitted_parts(steps[i], per) * rbs[i];
+        return n;
+    }
+};
 
 // first: the first 64 sequences.
 __device__ __forceinline__ int part_steps(const Attention &a, const Lane &first)
 {
-    int64_t total = wave_total((int64_t)first.steps * first.rbs);
-    for (int b0 = 64; b0 < a.n_seqs; b0 += 64) {
-        const Lane x = lane_sequence(a, b0);
-        total += wave_total((int64_t)x.steps * x.rbs);
+    if (!a.fit) {
+        int64_t total = wave_total((int64_t)first.steps * first.rbs);
+        for (int b0 = 64; b0 < a.n_seqs; b0 += 64) {
+            const Lane x = lane_sequence(a, b0);
+            total += wave_total((int64_t)x.steps * x.rbs);
+        }
+        return part_size(a, total);
     }
-    return a.fit ? fitted_steps(a, first, total) : part_size(a, total);
+    const int longest = (a.max_kv - 1) / kStep + 1;
+    if (a.n_seqs <= 64) {
+        auto count = [&](int per) { return wave_total((int64_t)fitted_parts(first.steps, per) * first.rbs); };
+        return fitted_steps(a, wave_total((int64_t)first.steps * first.rbs), count(longest), count);
+    }
+    Lanes all;
+    int64_t total = 0, blocks = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += Lanes::Most) {
+        all.load(a, b0);
+        total += all.total();
+        blocks += all.parts(longest);
+    }
+    auto count = [&](int per) {
+        int64_t n = 0;
+        if (a.n_seqs <= Lanes::Most) {
+            n = all.parts(per);
+        } else {
+            for (int b0 = 0; b0 < a.n_seqs; b0 += Lanes::Most) {
+                all.load(a, b0);
+                n += all.parts(per);
+            }
+        }
+        return wave_total(n);
+    };
+    return fitted_steps(a, wave_total(total), wave_total(blocks), count);
 }
 
 // Parts of a sequence: the nearest whole number (always rounding up would cut 880 row

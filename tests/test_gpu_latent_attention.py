@@ -197,3 +197,20 @@ def test_pages_beyond_32_bits(kvr):
     want = p @ x[:, :512].double()
     # weights and outputs rounded to 2^-8 of themselves
     assert float(((out[0].double() - want).abs() - 2.0 ** -8 * (want.abs() + 1.01 * p @ x[:, :512].double().abs())).max()) <= 0
+
+
+@pytest.mark.parametrize("fmt,heads,rank,n", [("bf16", 4, 256, 299), ("fp8", 20, 512, 150), ("fp16", 64, 256, 70),
+                                              ("bf16", 70, 512, 75), ("bf16", 3, 256, 1100)])
+def test_many_sequences_and_long_ones(kvr, fmt, heads, rank, n):
+    """More row blocks than half of the CUs: parts of several rounds, beside sequences that are not cut."""
+    rng = np.random.default_rng(n)
+    kv = [int(x) for x in np.exp(rng.uniform(0, np.log(60), n))]
+    kv[n // 2], kv[-1] = 9000, 3001
+    p = LatentProblem(kvr, 50 + n, fmt, kv, [1] * n, heads, rank, 32, 16)
+    p.check(*p.call(), rows=3)
+
+
+@pytest.mark.parametrize("n,tokens", [(130, 700), (200, 300), (260, 530)])
+def test_equal_sequences_of_several_rounds(kvr, n, tokens):
+    p = LatentProblem(kvr, n, "bf16", [tokens] * n, [1 + b % 2 for b in range(n)], 8, 256, 64, 64)
+    p.check(*p.call(), rows=3)

@@ -320,3 +320,24 @@ def test_offsets_beyond_32_bits(kvr):
     kvr.kvr_pages_copy(kvr.PageBuffers(kvr.LatentCache(rows, 64)),
                        torch.tensor([[last, last - 1]], dtype=torch.int32, device="cuda"))
     assert float(rows[last - 1].min()) == 3 and float(rows[last - 2].max()) == 0
+
+
+@pytest.mark.parametrize("shape", [(2048, 30, 90, 16), (2049, 30, 90, 16), (4096, 64, 80, 16), (4097, 20, 300, 16), (4096, 65, 80, 32),
+                                   (2048, 1024, 4, 16), (2048, 1025, 4, 16), (2000, 40, 1639, 16)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_random_runs_of_larger_pools(kvr, shape):
+    """Sizes about which the calls change from one launch to several."""
+    rng = np.random.default_rng(sum(shape))
+    n_pages, n_seqs, width, page = shape
+    width = min(width, 2 * n_pages // n_seqs)   # of the lengths that are asked for
+    x = Both(kvr, *shape)
+    for step in range(6):
+        new = rng.integers(0, width * page + 1, n_seqs)
+        x.resize(np.where(rng.random(n_seqs) < 0.3, 0, np.where(rng.random(n_seqs) < 0.5, -1, new)))
+        parent = np.where((x.m.len == 0) & (rng.random(n_seqs) < 0.8), rng.integers(0, n_seqs, n_seqs), -1)
+        parent[parent == np.arange(n_seqs)] = -1
+        x.fork(parent)
+        x.resize(np.where(rng.random(n_seqs) < 0.5, x.m.len + rng.integers(0, 2 * page, n_seqs), -1))
+        x.compact(None if step % 2 else 40)
+    x.resize(np.zeros(n_seqs, int))
+    assert x.m.refs.sum() == 0

@@ -63,6 +63,7 @@ __device__ __forceinline__ Part find_part(const Attention &a, int item)
     }
     Lane x = lane_sequence(a, 0);
     const int per = part_steps(a, x);
+    if (a.chosen && item == 0 && threadIdx.x == 0) *a.chosen = per;
     int base = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
         if (b0) x = lane_sequence(a, b0);

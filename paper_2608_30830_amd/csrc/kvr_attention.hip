@@ -28,7 +28,7 @@ __global__ __launch_bounds__(Threads) void combine_kernel(Attention a)
     const int rows = nq * a.group;
     if ((int)blockIdx.x * rows_per_block >= rows) return;
     Lane x = lane_sequence(a, 0);
-    const int per = part_steps(a, x);
+    const int per = a.chosen ? *a.chosen : part_steps(a, x);
     const int parts = parts_of(a, steps_of(len, nq), per);
     if (parts <= 1) return;
     int64_t base = 0;   // items before this sequence's

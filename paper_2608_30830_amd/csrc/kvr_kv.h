@@ -107,6 +107,8 @@ struct Attention {
     float *part_o;               // [items][heads][block_rows][dim]
     float4 *part_ml;             // [items][heads][block_rows]: maximum, sum of the weights, and
                                  // of the weights as rounded for the products
+    int32_t *chosen;             // where the first block leaves the steps of a part for the joining
+                                 // kernel (nullptr: that finds them itself)
     int *status;
 };
 

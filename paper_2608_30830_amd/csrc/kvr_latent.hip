@@ -32,7 +32,8 @@ size_t plan_latent_attention(LatentAttention &l)
         }
         return 0;
     }
-    return (size_t)a.max_items * a.block_rows * (l.c.rank + 4) * sizeof(float);
+    // and a word for the steps of a part
+    return (size_t)a.max_items * a.block_rows * (l.c.rank + 4) * sizeof(float) + 16;
 }
 
 hipError_t launch_latent_attention(const LatentAttention &l, hipStream_t stream)

@@ -166,6 +166,7 @@ int kvr_latent_attention(const kvr_latent_cache *cache, const kvr_sequences *seq
         const size_t cells = need / sizeof(float) / (size_t)(l.c.rank + 4);
         a.part_o = static_cast<float *>(d_ws);
         a.part_ml = reinterpret_cast<float4 *>(a.part_o + cells * (size_t)l.c.rank);
+        a.chosen = reinterpret_cast<int32_t *>(a.part_ml + cells);
     }
     KVR_TRY(kvr::kv::launch_latent_attention(l, static_cast<hipStream_t>(hip_stream)));
     return KVR_OK;

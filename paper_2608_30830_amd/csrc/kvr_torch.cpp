@@ -1,4 +1,4 @@
-// The KV cache's entry points on torch tensors: checks of types, shapes and strides,
+// The entry points of the caches and their pages on torch tensors: checks of types, shapes and strides,
 // outputs and workspaces from torch's allocator, torch's current stream, then the C ABI.
 // A call costs about what its launches cost: from Python, one launch takes 2.5 us,
 // reading the tensors and filling in the C arguments another 4 us through ctypes and

@@ -14,8 +14,10 @@ size_t plan_latent_attention(LatentAttention &l)
     const int64_t rows = (int64_t)a.max_q * a.group;
     const int64_t longest = cdiv(a.max_kv, kStep);
     // Registers hold 64 rows of 512 elements a block, or 128 of 256 (64 sequences of 16,384 tokens,
-    // 128 heads: 229 us in blocks of 128 rows, 334 in blocks of 64).
-    a.block_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 || l.c.rank == 512 ? 64 : 128;
+    // 128 heads: 229 us in blocks of 128 rows, 334 in blocks of 64); the rows of a sequence are divided
+    // evenly among as few blocks as that allows, in tiles of 16.
+    const int64_t most = rows <= 64 || l.c.rank == 512 ? 64 : 128;
+    a.block_rows = rows <= 16 ? 16 : (int32_t)(16 * cdiv(rows, 16 * cdiv(rows, most)));
     // (one sequence of 1,000 tokens: 17.3 us in parts of four steps, 19.7 of eight; with more rows a
     // part's way through memory costs as much as about eight steps)
     a.min_steps = rows <= 16 ? 4 : 8;

@@ -24,14 +24,16 @@
 // instructions are not in the cache, about 4: 1,000 tokens of one sequence take 14 us in 8 blocks.
 //
 // Beyond (ManyRows) the waves share tiles of 64 cached rows, one of two in LDS while the next one
-// is on its way.  A block has two groups of 16 RT rows, each of them two waves: for the scores they
-// divide the cached rows, for the outputs the columns, and exchange the weights through LDS.  So each
+// is on its way.  A block has groups of two waves, each with up to RT times 16 rows: for the scores
+// they divide the cached rows, for the outputs the columns, and exchange the weights through LDS.  So each
 // fragment that a wave reads meets all its rows, no wave reads the whole tile twice, and the
 // accumulators of a wave are half a row wide, which leaves registers to read LDS a group of
 // fragments ahead.  (Four waves of 32 rows each and no exchange: 483 us where this takes 276, 64
 // sequences of 8,192 tokens and 128 heads of 512 + 64.)  Reading LDS bounds it, with the matrix
 // instructions: 128 heads run at 650 TFLOP/s from one length to the next, of rank 256, where 128 rows
-// share what is read, at 760.  Loads made between the products, a few at a time, were slower: each
+// share what is read, at 760.  A wave works on the tiles of 16 rows that it has, and a group has its
+// second one when all have one: 144 rows of rank 256 over 131,071 tokens take 52 us in two blocks of 80 and 64,
+// where two of 128 and 16 took 61.  Loads made between the products, a few at a time, were slower: each
 // waits until the queue of loads has room.
 //
 // Each source that includes this header builds the kernels for one cache format.
@@ -727,7 +729,7 @@ template <int FMT, int RK, int RO, int RT, int WAVES>
 struct ManyRows : LatentTile<FMT, RK, RO, 64, WAVES> {
     using T = LatentTile<FMT, RK, RO, 64, WAVES>;
     using T::a, T::n, T::g, T::lane, T::len, T::prefix, T::rows;
-    static constexpr int MT = T::MT, NB = T::NB, Waves = WAVES, BlockRows = Waves / 2 * 16 * RT;
+    static constexpr int MT = T::MT, NB = T::NB, Waves = WAVES, Groups = Waves / 2, BlockRows = Groups * 16 * RT;
     static constexpr int VT = RK;   // value tiles of a wave: half of the columns
     static constexpr int Group = WAVES == 4 ? 8 : RT == 2 ? 2 : 4;   // fragments, as registers allow
     // LDS: two tiles, the weights that waves exchange, what they say about their references
@@ -741,22 +743,35 @@ struct ManyRows : LatentTile<FMT, RK, RO, 64, WAVES> {
 
     __device__ ManyRows(const LatentAttention &la) : T(la) {}
 
-    // Step k of the block: rows t to t + 63, before `end`.
-    __device__ __forceinline__ bool compute(int k, int t, int end, int row0, bool active, char *tile, char *lds)
+    // Row of the block's that lane n has in this wave's tile r: the tiles of a group are as many rows
+    // apart as all groups have, so that each has one before any has two.
+    __device__ __forceinline__ int row_in_block(int r) const { return 16 * ((wave >> 1) + Groups * r) + n; }
+
+    // Step k of the block: rows t to t + 63, before `end`.  R: this wave's tiles with any rows.
+    template <int R>
+    __device__ __forceinline__ bool compute(int k, int t, int end, int r0, char *tile, char *lds)
     {
+        uint32_t *flag = reinterpret_cast<uint32_t *>(lds + FlagAt) + (k & 1);
+        if constexpr (R == 0) {   // the others' barriers
+            block_barrier();
+            if (*flag == (uint32_t)k + 1) {
+                block_barrier();
+                block_barrier();
+            }
+            return false;
+        } else {
         uint32_t key_at = T::key_at, tail_at = T::tail_at, val_at = T::val_at;
         asm volatile("" : "+v"(key_at), "+v"(tail_at), "+v"(val_at));
         const bool hides = t + 64 > prefix || t + 64 > end;
         // this wave's rows for the scores, and columns for the outputs
         const char *mine = tile + side * 32 * T::Rank * 2, *mine_tail = tile + side * 32 * 64 * RO;
         const char *half = tile + side * (T::Rank / 16 >> 3) * 128;
-        const bool odd = hides && active && T::template has_odd<T::Rank / 16>(tile, side * (T::Rank / 16));
-        f32x4 sc[RT][2];
-        u32x4 pv[RT][2];   // weights of the first and the second 32 rows
-        static_for<0, 2 * RT>([&](auto I) {
+        const bool odd = hides && T::template has_odd<T::Rank / 16>(tile, side * (T::Rank / 16));
+        f32x4 sc[R][2];
+        u32x4 pv[R][2];   // weights of the first and the second 32 rows
+        static_for<0, 2 * R>([&](auto I) {
             sc[decltype(I)::value / 2][decltype(I)::value % 2] = f32x4{0, 0, 0, 0};
         });
-        uint32_t *flag = reinterpret_cast<uint32_t *>(lds + FlagAt) + (k & 1);
         u32x4 *shared = reinterpret_cast<u32x4 *>(lds + WeightsAt) + lane;
         auto load = [&](auto K) {
             constexpr int f = decltype(K)::value, e = f - 2 * NB;   // e: tile, then half of the rows
@@ -766,41 +781,41 @@ struct ManyRows : LatentTile<FMT, RK, RO, 64, WAVES> {
         };
         auto key = [&](auto K, u32x4 x) {
             constexpr int f = decltype(K)::value;
-            static_for<0, RT>([&](auto R) {
-                constexpr int r = decltype(R)::value;
+            static_for<0, R>([&](auto I) {
+                constexpr int r = decltype(I)::value;
                 sc[r][f % 2] = mfma<MT>(x, q[r][f / 2], sc[r][f % 2]);
             });
         };
         auto middle = [&] {
-            float top[RT], sum[RT], rounded[RT];
+            float top[R], sum[R], rounded[R];
             bool moves = false;
-            static_for<0, RT>([&](auto R) {
-                constexpr int r = decltype(R)::value;
-                if (hides) T::hide(T::query_of(row0 + 16 * r + n), t + 32 * side + 4 * g, end, sc[r]);
+            static_for<0, R>([&](auto I) {
+                constexpr int r = decltype(I)::value;
+                if (hides) T::hide(T::query_of(r0 + row_in_block(r)), t + 32 * side + 4 * g, end, sc[r]);
                 top[r] = T::largest(sc[r]);
                 moves = moves || top[r] > m[r] + (8.0f + T::kBelow);
             });
             auto weigh = [&] {
-                static_for<0, RT>([&](auto R) {
-                    constexpr int r = decltype(R)::value;
+                static_for<0, R>([&](auto I) {
+                    constexpr int r = decltype(I)::value;
                     const u32x4 p = T::weights(sc[r], m[r], sum[r], rounded[r]);
                     shared[(wave * RT + r) * 64] = p;
                     pv[r][0] = p;
                 });
             };
             weigh();
-            if (__ballot(moves && active) && lane == 0) *flag = (uint32_t)k + 1;
+            if (__ballot(moves) && lane == 0) *flag = (uint32_t)k + 1;
             block_barrier();
             if (*flag == (uint32_t)k + 1) {   // some reference moves: the two waves of a row agree on theirs
                 float *rm = reinterpret_cast<float *>(lds + MaxAt);
-                static_for<0, RT>([&](auto R) {
-                    constexpr int r = decltype(R)::value;
+                static_for<0, R>([&](auto I) {
+                    constexpr int r = decltype(I)::value;
                     top[r] = row_max(top[r]);
                     if (g == 0) rm[(wave * RT + r) * 16 + n] = top[r];
                 });
                 block_barrier();
-                static_for<0, RT>([&](auto R) {
-                    constexpr int r = decltype(R)::value;
+                static_for<0, R>([&](auto I) {
+                    constexpr int r = decltype(I)::value;
                     const float x = fmaxf(fmaxf(top[r], rm[((wave ^ 1) * RT + r) * 16 + n]) - T::kBelow, m[r]);
                     const float f = __builtin_amdgcn_exp2f(m[r] - x);
                     l[r] *= f;
@@ -811,8 +826,8 @@ struct ManyRows : LatentTile<FMT, RK, RO, 64, WAVES> {
                 weigh();
                 block_barrier();
             }
-            static_for<0, RT>([&](auto R) {
-                constexpr int r = decltype(R)::value;
+            static_for<0, R>([&](auto I) {
+                constexpr int r = decltype(I)::value;
                 l[r] += sum[r];
                 w[r] += rounded[r];
                 const u32x4 other = shared[((wave ^ 1) * RT + r) * 64], own = pv[r][0];
@@ -825,13 +840,14 @@ struct ManyRows : LatentTile<FMT, RK, RO, 64, WAVES> {
         };
         auto val = [&](auto E, u32x4 x) {
             constexpr int e = decltype(E)::value;
-            static_for<0, RT>([&](auto R) {
-                constexpr int r = decltype(R)::value;
+            static_for<0, R>([&](auto I) {
+                constexpr int r = decltype(I)::value;
                 o[r][e / 2] = mfma<MT>(x, pv[r][e & 1], o[r][e / 2]);
             });
         };
         fragments<Group, 2 * NB, 2 * VT>(load, key, middle, val);
         return odd;
+        }
     }
 
     __device__ __forceinline__ void run(char *lds)
@@ -840,11 +856,12 @@ struct ManyRows : LatentTile<FMT, RK, RO, 64, WAVES> {
         if (p.b < 0) return;
         T::begin(p);
         wave = uniform((int)(threadIdx.x >> 6)), side = wave & 1;
-        const int r0 = p.rb * BlockRows, row0 = r0 + (wave >> 1) * 16 * RT;
+        const int r0 = p.rb * a.block_rows, mine = min(a.block_rows, rows - r0);   // the block's rows
+        const int tiles = min(RT, (mine - 16 * (wave >> 1) + 16 * Groups - 1) / (16 * Groups));   // of this wave
         const int first = p.first * kStep, end = min(len, p.last * kStep);
         const int steps = (end - first + 63) / 64;
         const uint32_t lds_at = lds_address(lds);
-        static_for<0, RT>([&](auto R) { T::load_query(row0 + 16 * decltype(R)::value + n, q[decltype(R)::value]); });
+        static_for<0, RT>([&](auto R) { T::load_query(r0 + row_in_block(decltype(R)::value), q[decltype(R)::value]); });
         T::hold(p.first * kStep >> a.c.page_shift);
         typename T::Codes c;
         if constexpr (T::Quant) T::fetch_codes(T::locate(first, end, wave), wave, c);
@@ -856,22 +873,27 @@ struct ManyRows : LatentTile<FMT, RK, RO, 64, WAVES> {
             m[r] = kLowest, l[r] = 0.0f, w[r] = 0.0f;
             static_for<0, VT>([&](auto E) { o[r][decltype(E)::value] = f32x4{0, 0, 0, 0}; });
         });
-        const bool active = row0 < rows;
         bool odd = false;
-        for (int k = 0; k < steps; ++k) {
-            const int t = first + 64 * k;
-            char *tile = lds + (k & 1) * T::Tile;
-            if constexpr (T::Quant) {
-                T::put_codes(c, wave, tile);
-                if (k + 1 < steps) T::fetch_codes(T::locate(t + 64, end, wave), wave, c);
-            } else {
-                wait_loads<0>();
+        auto loop = [&](auto R) {
+            for (int k = 0; k < steps; ++k) {
+                const int t = first + 64 * k;
+                char *tile = lds + (k & 1) * T::Tile;
+                if constexpr (T::Quant) {
+                    T::put_codes(c, wave, tile);
+                    if (k + 1 < steps) T::fetch_codes(T::locate(t + 64, end, wave), wave, c);
+                } else {
+                    wait_loads<0>();
+                }
+                block_barrier();   // the step's rows are there, the other tile has been read
+                if constexpr (!T::Quant)
+                    if (k + 1 < steps) T::fetch(T::locate(t + 64, end, wave), wave, lds_at + ((k + 1) & 1) * T::Tile);
+                odd |= compute<decltype(R)::value>(k, t, end, r0, tile, lds);
             }
-            block_barrier();   // the step's rows are there, the other tile has been read
-            if constexpr (!T::Quant)
-                if (k + 1 < steps) T::fetch(T::locate(t + 64, end, wave), wave, lds_at + ((k + 1) & 1) * T::Tile);
-            odd |= compute(k, t, end, row0, active, tile, lds);
-        }
+        };
+        // (loops of their own, or the registers of all are live in each; the barriers are the same)
+        if (RT == 2 && tiles == 2) loop(std::integral_constant<int, RT>{});
+        else if (tiles > 0) loop(std::integral_constant<int, 1>{});
+        else loop(std::integral_constant<int, 0>{});
         __syncthreads();   // LDS may be used for other things
         odd = block_any(odd, reinterpret_cast<uint32_t *>(lds + FlagAt));
         // the sums of a row's two waves
@@ -888,18 +910,18 @@ struct ManyRows : LatentTile<FMT, RK, RO, 64, WAVES> {
         __syncthreads();
         static_for<0, RT>([&](auto R) {
             constexpr int r = decltype(R)::value;
-            const int row = row0 - r0 + 16 * r + n;
-            if (r0 + row >= rows) return;
+            const int row = row_in_block(r);
+            if (row >= mine) return;
             const float sum = l[r] + sums[(2 * (wave ^ 1) * RT + r) * 16 + n];
             const float norm = w[r] + sums[((2 * (wave ^ 1) + 1) * RT + r) * 16 + n];
             const float inv = norm == 0.0f ? 0.0f : 1.0f / norm;
             static_for<0, VT>([&](auto E) {
                 constexpr int e = decltype(E)::value;
-                T::store(p, r0, row, BlockRows, side * (T::Rank / 2) + 16 * e + 4 * g, o[r][e], inv);
+                T::store(p, r0, row, a.block_rows, side * (T::Rank / 2) + 16 * e + 4 * g, o[r][e], inv);
             });
-            if (side == 0 && g == 0) T::store_sums(p, r0, row, BlockRows, m[r], sum, norm);
+            if (side == 0 && g == 0) T::store_sums(p, r0, row, a.block_rows, m[r], sum, norm);
         });
-        if (odd) T::put_odd(p, r0, BlockRows);
+        if (odd) T::put_odd(p, r0, a.block_rows);
     }
 };
 
@@ -915,7 +937,7 @@ __global__ __launch_bounds__(64 * K::Waves, K::Waves / 4) void latent_kernel(Lat
 template <class K>
 hipError_t launch_latent_kernel(const LatentAttention &l, dim3 grid, hipStream_t stream)
 {
-    if (l.a.block_rows != K::BlockRows) return hipErrorInvalidValue;
+    if (l.a.block_rows > K::BlockRows) return hipErrorInvalidValue;
     latent_kernel<K><<<grid, 64 * K::Waves, 0, stream>>>(l);
     return hipGetLastError();
 }
@@ -923,14 +945,12 @@ hipError_t launch_latent_kernel(const LatentAttention &l, dim3 grid, hipStream_t
 template <int FMT, int RK, int RO>
 hipError_t launch_latent_rows(const LatentAttention &l, dim3 grid, hipStream_t stream)
 {
-    switch (l.a.block_rows) {   // as plan_latent_attention chose
-    case 16: return launch_latent_kernel<FewRows<FMT, RK, RO>>(l, grid, stream);
-    case 32: return launch_latent_kernel<ManyRows<FMT, RK, RO, 1, 4>>(l, grid, stream);
-    case 64: return launch_latent_kernel<ManyRows<FMT, RK, RO, 1, 8>>(l, grid, stream);
-    default:
-        if constexpr (RK == 8) return launch_latent_kernel<ManyRows<FMT, RK, RO, 2, 8>>(l, grid, stream);
-        else return hipErrorInvalidValue;
-    }
+    const int n = l.a.block_rows;   // as plan_latent_attention chose
+    if (n <= 16) return launch_latent_kernel<FewRows<FMT, RK, RO>>(l, grid, stream);
+    if (n <= 32) return launch_latent_kernel<ManyRows<FMT, RK, RO, 1, 4>>(l, grid, stream);
+    if (n <= 64) return launch_latent_kernel<ManyRows<FMT, RK, RO, 1, 8>>(l, grid, stream);
+    if constexpr (RK == 8) return launch_latent_kernel<ManyRows<FMT, RK, RO, 2, 8>>(l, grid, stream);
+    else return hipErrorInvalidValue;
 }
 
 template <int FMT>

@@ -214,3 +214,23 @@ def test_many_sequences_and_long_ones(kvr, fmt, heads, rank, n):
 def test_equal_sequences_of_several_rounds(kvr, n, tokens):
     p = LatentProblem(kvr, n, "bf16", [tokens] * n, [1 + b % 2 for b in range(n)], 8, 256, 64, 64)
     p.check(*p.call(), rows=3)
+
+
+@pytest.mark.parametrize("fmt,rank", [("bf16", 256), ("fp16", 256), ("fp8", 256), ("bf16", 512), ("fp8", 512)])
+@pytest.mark.parametrize("heads,q", [(12, 4), (24, 3), (16, 5), (20, 4), (13, 10), (16, 9), (59, 3), (20, 13)])
+def test_rows_divided_among_blocks(kvr, fmt, rank, heads, q):
+    """Rows that fill no whole block, of sequences that have more and fewer of them, with trees, and a
+    hidden latent that is not finite."""
+    import torch
+    p = LatentProblem(kvr, 7 * heads + q, fmt, [q + 30, 700, 1 + q // 2, 333], [q, q, 1 + q // 2, 1], heads, rank, 64, 16, tree=True)
+    p.check(*p.call(), rows=60)
+    if fmt == "fp8":
+        return
+    # the last token of the second sequence, which only its own query sees
+    t = torch.arange(q, device="cuda")
+    p.mask[int(p.cu[1]):int(p.cu[2]), 0] = (2 << t) - 1
+    p.rows[int(p.first[2]) - 1, 3] = float("nan")
+    p.write()
+    out, lse = p.call()
+    assert bool(torch.isnan(out[int(p.cu[2]) - 1]).any()) and not bool(torch.isnan(out[:int(p.cu[2]) - 1]).any())
+    p.check(out, lse, rows=30)

@@ -286,3 +286,43 @@ def test_captured_calls(kvr):
         torch.cuda.synchronize()
         for x, y, z in zip(got, want, eager):
             assert torch.equal(x, y) and torch.equal(z, y)
+
+
+def test_two_graphs_that_share_a_workspace(kvr):
+    """Replayed in turn on one stream, with eager calls on the same workspace between."""
+    import torch
+    p = LatentProblem(kvr, 81, "bf16", [3000, 700], [1, 3], 40, 512, 64, 64)
+    s = LatentProblem(kvr, 82, "fp8", [9000], [1], 16, 512, 64, 16)
+    x = PromptProblem(83, "bf16", [50], [5000], 4, 2, 128, 64)
+    ws = torch.full((1 << 26,), 0xFF, dtype=torch.uint8, device="cuda")
+    calls = [lambda: p.call(workspace=ws, check=False), lambda: (*s.call(workspace=ws, check=False), *x.call(kvr, workspace=ws, check=False))]
+    want = [c() for c in calls]
+    graphs, got = [], []
+    for c in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            got.append(c())
+    for i in range(3):
+        for g, out, ref, other in zip(graphs, got, want, calls[::-1]):
+            for t in out:
+                t.zero_()
+            ws.fill_(i)
+            if i:
+                other()
+            g.replay()
+            assert all(torch.equal(a, b) for a, b in zip(out, ref))
+
+
+def test_calls_at_the_same_time(kvr):
+    """On four streams, with workspaces of their own."""
+    import torch
+    p = [LatentProblem(kvr, 90 + i, f, [4000 + 500 * i] * 3, [2] * 3, h, r, 64, 64)
+         for i, (f, h, r) in enumerate([("bf16", 8, 512), ("fp8", 40, 256), ("fp16", 70, 256), ("bf16", 30, 512)])]
+    want = [x.call() for x in p]
+    streams = [torch.cuda.Stream() for _ in p]
+    torch.cuda.synchronize()
+    got = [[x.call(stream=s, check=False) for _ in range(5)] for x, s in zip(p, streams)]
+    torch.cuda.synchronize()
+    for w, each in zip(want, got):
+        for g in each:
+            assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1])

@@ -43,6 +43,7 @@ hipError_t launch_latent_read(const LatentRead &a, hipStream_t stream);
 struct LatentAttention {
     Attention a;
     Latents c;
+    int32_t span;   // row blocks of a part, about
 };
 // Fills the launch plan; returns the workspace bytes (0: no sequence is cut).
 size_t plan_latent_attention(LatentAttention &l);

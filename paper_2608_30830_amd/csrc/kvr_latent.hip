@@ -21,6 +21,7 @@ size_t plan_latent_attention(LatentAttention &l)
     // (one sequence of 1,000 tokens: 17.3 us in parts of four steps, 19.7 of eight; with more rows a
     // part's way through memory costs as much as about eight steps)
     a.min_steps = rows <= 16 ? 4 : 8;
+    l.span = (int32_t)std::min<int64_t>(cdiv(rows, a.block_rows), 32);   // an XCD has 32 CUs
     const int64_t blocks = std::min<int64_t>((int64_t)a.n_seqs * cdiv(rows, a.block_rows),
                                              a.n_queries * a.group / a.block_rows + a.n_seqs);
     a.target = kSlots;

@@ -150,7 +150,7 @@ struct LatentTile {
     const LatentAttention &la;
     const Attention &a;
     const int n, g, lane;
-    int len, prefix, q0, rows;
+    int item, len, prefix, q0, rows;
     const int32_t *pages;
     int held, held_at;   // entries held_at on of the sequence's row of the page table, one a lane
     uint32_t key_at, tail_at, val_at;   // byte offsets of this lane in a tile
@@ -167,6 +167,16 @@ struct LatentTile {
         tail_at = Main + n * (64 * RO) + ((g ^ tail_swizzle(n)) << 4);
         const int r = 4 * g + (n >> 2);
         val_at = r * (Rank * 2) + (((n & 3) >> 1 ^ r) << 4) + ((n & 1) << 3);
+    }
+    // What this block works on.  A part's row blocks read the same cached rows: they are on one XCD
+    // (blocks go to the eight in turn), at the same time, so that its cache has them for all but one.
+    // (Four sequences of 32,768 tokens, 144 rows of rank 512: 87 us, with the parts' blocks in a row 90.)
+    __device__ __forceinline__ Part find()
+    {
+        const int b = blockIdx.x, whole = la.span > 1 ? gridDim.x / (8 * la.span) * (8 * la.span) : 0;
+        const int j = b >> 3;
+        item = b < whole ? ((j / la.span << 3) + (b & 7)) * la.span + j % la.span : b;
+        return find_part(a, item);
     }
     __device__ __forceinline__ void begin(const Part &p)
     {
@@ -477,7 +487,7 @@ struct LatentTile {
                                           float inv) const
     {
         if (p.parts != 1) {
-            *reinterpret_cast<f32x4 *>(a.part_o + ((int64_t)blockIdx.x * block_rows + row) * Rank + d) = x;
+            *reinterpret_cast<f32x4 *>(a.part_o + ((int64_t)item * block_rows + row) * Rank + d) = x;
             return;
         }
         const int i0 = (r0 + row) / a.group, head = r0 + row - i0 * a.group;
@@ -488,7 +498,7 @@ struct LatentTile {
                                                float sum, float norm) const
     {
         if (p.parts != 1) {
-            a.part_ml[(int64_t)blockIdx.x * block_rows + row] = float4{top, sum, norm, 0.0f};
+            a.part_ml[(int64_t)item * block_rows + row] = float4{top, sum, norm, 0.0f};
         } else if (a.lse) {
             const int i0 = (r0 + row) / a.group, head = r0 + row - i0 * a.group;
             a.lse[(int64_t)(q0 + i0) * a.q_heads + head] =
@@ -527,7 +537,7 @@ struct LatentTile {
             for (int t = max(p.first, prefix / kStep) * kStep; t < t1; ++t) {
                 if (!sees(i0, t - prefix) || !odd_at(t, d)) continue;
                 if (p.parts != 1) {
-                    a.part_o[((int64_t)blockIdx.x * block_rows + row) * Rank + d] = __uint_as_float(0x7fc00000u);
+                    a.part_o[((int64_t)item * block_rows + row) * Rank + d] = __uint_as_float(0x7fc00000u);
                 } else {
                     const int head = r0 + row - i0 * a.group;
                     uint16_t *y = reinterpret_cast<uint16_t *>(a.out.p) +
@@ -642,7 +652,7 @@ struct FewRows : LatentTile<FMT, RK, RO, 32, 1> {
 
     __device__ __forceinline__ void run(char *lds)
     {
-        const Part p = find_part(a, (int)blockIdx.x);
+        const Part p = T::find();
         if (p.b < 0) return;
         T::begin(p);
         const int wave = uniform((int)(threadIdx.x >> 6));
@@ -852,7 +862,7 @@ struct ManyRows : LatentTile<FMT, RK, RO, 64, WAVES> {
 
     __device__ __forceinline__ void run(char *lds)
     {
-        const Part p = find_part(a, (int)blockIdx.x);
+        const Part p = T::find();
         if (p.b < 0) return;
         T::begin(p);
         wave = uniform((int)(threadIdx.x >> 6)), side = wave & 1;

@@ -234,3 +234,9 @@ def test_rows_divided_among_blocks(kvr, fmt, rank, heads, q):
     out, lse = p.call()
     assert bool(torch.isnan(out[int(p.cu[2]) - 1]).any()) and not bool(torch.isnan(out[:int(p.cu[2]) - 1]).any())
     p.check(out, lse, rows=30)
+
+
+@pytest.mark.parametrize("rank,heads,q", [(512, 64, 40), (256, 128, 37), (512, 128, 17)])
+def test_more_row_blocks_than_an_xcd_has(kvr, rank, heads, q):
+    p = LatentProblem(kvr, rank + q, "bf16", [900, 333, q], [q, 1, q], heads, rank, 64, 64)
+    p.check(*p.call(), rows=60)

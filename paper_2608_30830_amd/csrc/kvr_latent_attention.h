@@ -525,16 +525,19 @@ struct LatentTile {
     }
     // What was taken out of the products where tokens are hidden, to the block's rows that see it,
     // after they have been stored.  The same element was part of the score: that is an infinity or a
-    // NaN too, the weight 0 or NaN, and their product NaN.
+    // NaN too, the weight 0 or NaN, and their product NaN.  A tile is cleared whole if it holds a token
+    // that some query may not see, or ends past the part: all of the part's tokens are looked at from
+    // the first such tile on, older ones among them.
     __device__ __forceinline__ void put_odd(const Part &p, int r0, int block_rows) const
     {
         wait_loads<0>();   // of stores too
         __syncthreads();
-        const int t1 = min(len, p.last * kStep);
+        const int t0 = p.first * kStep, t1 = min(len, p.last * kStep);
+        const int from = t0 + max(0, min(prefix, t1) - t0) / TileRows * TileRows;
         for (int i = threadIdx.x; i < min(block_rows, rows - r0) * Rank; i += blockDim.x) {
             const int row = i / Rank, d = i - row * Rank;
             const int i0 = (r0 + row) / a.group;
-            for (int t = max(p.first, prefix / kStep) * kStep; t < t1; ++t) {
+            for (int t = from; t < t1; ++t) {
                 if (!sees(i0, t - prefix) || !odd_at(t, d)) continue;
                 if (p.parts != 1) {
                     a.part_o[((int64_t)item * block_rows + row) * Rank + d] = __uint_as_float(0x7fc00000u);

@@ -5,7 +5,8 @@ import math
 import numpy as np
 import pytest
 
-from tests.latent_problem import LatentProblem
+from tests.latent_problem import LatentProblem, check_rows
+from tests.test_gpu_kv_cache import _np
 
 pytestmark = pytest.mark.gpu
 
@@ -240,3 +241,48 @@ def test_rows_divided_among_blocks(kvr, fmt, rank, heads, q):
 def test_more_row_blocks_than_an_xcd_has(kvr, rank, heads, q):
     p = LatentProblem(kvr, rank + q, "bf16", [900, 333, q], [q, 1, q], heads, rank, 64, 64)
     p.check(*p.call(), rows=60)
+
+
+@pytest.mark.parametrize("heads,rank,q", [(4, 512, 1), (16, 256, 1), (20, 512, 1), (64, 512, 1), (64, 256, 1), (128, 512, 1),
+                                          (128, 256, 1), (20, 256, 7), (6, 512, 9)])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_seen_infinities_everywhere(kvr, fmt, heads, rank, q):
+    """One infinity in each 32 tokens of the past, each in a column of its own, whole parts of odd
+    numbers of steps and tiles that hold the first new token among them.  Their scores are -infinity,
+    so that they have no weight, and give NaN in those columns and nowhere else; for head 0 they are
+    infinity, and everything is NaN."""
+    import torch
+    p = LatentProblem(kvr, 60 + heads, fmt, [32 * (rank - 9), 100, 64 + q, 1000, 224], [q] * 5, heads, rank, 64, 16)
+    sign = 1 - 2 * (torch.arange(rank, device="cuda") % 2)
+    x = p.q[..., :rank]
+    x.copy_(x.abs().clamp(min=0.05) * sign)
+    x[:, 0] = -x[:, 0]
+    for b, t in enumerate(p.kv):
+        s = torch.arange(-(-t // 32), device="cuda")
+        at = 32 * s + 7 * s % 32
+        s, at = s[at < t - q], at[at < t - q]
+        slot = p.slots[int(p.first[b]) + at]
+        page, off = slot // 16, slot % 16
+        if fmt == "fp8":   # two times 2^127, alone in its block
+            for i in range(32):
+                p.cache.rows[page, off, s // 32 * 32 + i] = 0
+            p.cache.rows[page, off, s] = torch.where(sign[s] > 0, 0xC0, 0x40).to(torch.uint8)
+            p.cache.scale[page, off, s // 32] = 254
+        else:
+            p.cache.rows[page, off, s] = (-sign[s] * math.inf).to(p.cache.rows.dtype)
+    out, lse = (_np(x) for x in p.call())
+    rows, queries = _np(kvr.kvr_latent_read(p.cache, p.slots, torch.float32)), _np(p.q)
+    for b, (t, n) in enumerate(zip(p.kv, p.nq)):
+        xx, seen = rows[p.first[b]:p.first[b + 1]], p.seen(b)
+        odd = ~np.isfinite(xx)
+        gone, columns = odd.any(1), odd.any(0)[:rank]
+        assert gone.sum() == columns.sum() >= (t - q) // 32 and not odd[:, rank:].any()
+        seen = seen & ~gone
+        for i in range(n):
+            at = int(p.cu[b]) + i
+            assert np.isnan(out[at, 0]).all(), (b, i)
+            assert np.array_equal(np.isnan(out[at, 1:]), np.broadcast_to(columns, (heads - 1, rank))), (b, i)
+        for h in {1, heads // 2, heads - 1}:
+            own = slice(p.cu[b], p.cu[b + 1])
+            check_rows(out[own, h][:, ~columns], lse[own, h], queries[own, h], xx, xx[:, :rank][:, ~columns], seen, p.scale,
+                       p.dim, p.dtype, "fp16" if fmt == "fp16" else "bf16", (b, h))

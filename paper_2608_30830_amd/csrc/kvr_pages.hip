@@ -38,29 +38,33 @@ __device__ __forceinline__ bool in_pool(const Pool &p, int page)
     return page >= 0 && page < p.n_pages;
 }
 
-// A row gives a page back.
+// A row gives a page back that it held when the call began.
 __device__ __forceinline__ void give_back(const Pool &p, int page)
 {
-    if (!in_pool(p, page)) {
-        report(p);
-    } else if (atomicSub(p.refs + page, 1) <= 0) {
+    if (atomicSub(p.refs + page, 1) <= 0) {
         atomicAdd(p.refs + page, 1);
         report(p);
     }
 }
-// Up to four entries, which become -1: the atomics of one wait together.
-__device__ __forceinline__ void give_back(const Pool &p, int32_t *const (&at)[4])
+// Up to four entries, which become -1: the atomics of one wait together.  free: the pages that were
+// free when the call began, as bits.  What names one of them is reported, whether or not another row
+// has taken the page meanwhile, whose count it would lower.
+__device__ __forceinline__ void give_back(const Pool &p, const uint64_t *free, int32_t *const (&at)[4])
 {
     int page[4], held[4];
+    bool counts[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) page[k] = at[k] ? *at[k] : 0;
+    for (int k = 0; k < 4; ++k) page[k] = at[k] ? *at[k] : -1;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) held[k] = at[k] && in_pool(p, page[k]) ? atomicSub(p.refs + page[k], 1) : 0;
+    for (int k = 0; k < 4; ++k)
+        counts[k] = in_pool(p, page[k]) && !(free[page[k] >> 6] >> (page[k] & 63) & 1);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) held[k] = counts[k] ? atomicSub(p.refs + page[k], 1) : 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         if (!at[k]) continue;
-        if (held[k] <= 0) {   // outside the pool, or given back more often than held
-            if (in_pool(p, page[k])) atomicAdd(p.refs + page[k], 1);
+        if (held[k] <= 0) {   // outside the pool, free, or given back more often than held
+            if (counts[k]) atomicAdd(p.refs + page[k], 1);
             report(p);
         }
         *at[k] = -1;
@@ -238,7 +242,7 @@ __device__ __forceinline__ void finish_row(const Resize &r, int b, const Row &x,
             int32_t *at[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) at[k] = i + k * 64 < x.first ? row + i + k * 64 : nullptr;
-            give_back(p, at);
+            give_back(p, r.free, at);
         }
     }
 }
@@ -370,7 +374,7 @@ __global__ __launch_bounds__(kWide) void resize_small_kernel(Resize r)
             const int of = row_of_rank(p.n_seqs, i, [&](int j) { return (int64_t)back[j]; });
             at[k] = p.table + (int64_t)of * p.stride + rows[of].need + (i - back[of]);
         }
-        give_back(p, at);
+        give_back(p, free, at);
     }
     if (b < p.n_seqs) end_row(r, b, x, all);
 }

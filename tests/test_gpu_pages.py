@@ -341,3 +341,29 @@ def test_random_runs_of_larger_pools(kvr, shape):
         x.compact(None if step % 2 else 40)
     x.resize(np.zeros(n_seqs, int))
     assert x.m.refs.sum() == 0
+
+
+@pytest.mark.parametrize("n_pages", [300, 2048, 3000, 40000])
+def test_a_free_page_given_back_while_it_is_taken(kvr, n_pages):
+    """A row that names free pages ends, and one that takes these pages grows in the same call: the
+    first is reported, the second has them."""
+    import torch
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    n = min(n_pages, 1500) - 5
+    table = torch.full((4, n), -1, dtype=torch.int32, device="cuda")
+    for _ in range(5):
+        refs = torch.zeros(n_pages, dtype=torch.int32, device="cuda")
+        refs[:3] = 2                              # of rows that are not in the table
+        table[0] = torch.arange(n - 1, -1, -1, device="cuda") + 3
+        table[2] = table[0]
+        table[2, 0] = 1                           # a page that it does hold
+        kv, copies = ints(16 * n, 0, 16 * n, 0), None
+        for check in (False, True):               # the second call finds all in order
+            status = ints(0)
+            new = ints(0, 16 * n - 3, 0, -1)
+            copies = kvr.kvr_pages_resize(refs, table, kv, new, 16, copies=copies, status=status, check=check)
+            assert int(status.item()) == (0 if check else kvr.KVR_E_DOMAIN)
+            assert kv.tolist() == [0, 16 * n - 3, 0, 0] and bool((copies == -1).all())
+            assert refs[:3].tolist() == [2, 1, 2] and bool((refs[3:3 + n] == 1).all()) and not refs[3 + n:].any()
+            assert torch.equal(table[1], torch.arange(n, device="cuda").int() + 3)
+            assert bool((table[0] == -1).all()) and bool((table[2] == -1).all())

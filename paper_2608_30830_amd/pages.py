@@ -90,14 +90,20 @@ def kvr_pages_resize(refs, page_table, kv_len, new_len, page_size: int, copies=N
     Pages are taken lowest first, in the order of rows.  A row that grows and whose last, partly
     filled page is held by others too takes one in its place: returns ``copies`` [n_seqs, 2] int32,
     the pages to copy for each row (kvr_pages_copy, before the row is written to), or -1.  A row
-    that the free pages are too few for stays as it is (with ``check``: an error)."""
+    that the free pages are too few for stays as it is: with ``check`` an error, whose ``copies`` are
+    those of the rows that did grow."""
     c = kv._context()
     if check:
         status = kv._status(c, refs, check, status, stream)
     rc, copies, ws = c.fast.pages_resize(refs, page_table, kv_len, new_len, page_size, copies, workspace,
                                          status, kv._handle(stream))
     if rc or check or stream is not None:
-        kv._finish(c, "kvr_pages_resize", rc, check, status, stream, copies, ws)
+        try:
+            kv._finish(c, "kvr_pages_resize", rc, check, status, stream, copies, ws)
+        except c.pkg.KvrError as e:   # of the device: the other rows have their new pages
+            if not rc:
+                e.copies = copies
+            raise
     return copies
 
 
@@ -106,14 +112,20 @@ def kvr_pages_compact(refs, page_table, kv_len, page_size: int, max_moves: Optio
                       check: bool = True):
     """The highest pages in use into the lowest free ones, while those are lower and at most
     ``max_moves`` (all that there are by default).  Returns (``moves`` [max_moves, 2] int32, the pages to
-    copy, -1 from the last on; ``used`` [1] int32, the pages in use)."""
+    copy, -1 from the last on; ``used`` [1] int32, the pages in use).  With ``check`` a row that does not
+    fit is an error, whose ``moves`` and ``used`` are what was done all the same."""
     c = kv._context()
     if check:
         status = kv._status(c, refs, check, status, stream)
     rc, moves, used, ws = c.fast.pages_compact(refs, page_table, kv_len, page_size, max_moves, moves, used,
                                                workspace, status, kv._handle(stream))
     if rc or check or stream is not None:
-        kv._finish(c, "kvr_pages_compact", rc, check, status, stream, moves, used, ws)
+        try:
+            kv._finish(c, "kvr_pages_compact", rc, check, status, stream, moves, used, ws)
+        except c.pkg.KvrError as e:
+            if not rc:
+                e.moves, e.used = moves, used
+            raise
     return moves, used
 
 

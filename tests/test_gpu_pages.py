@@ -367,3 +367,30 @@ def test_a_free_page_given_back_while_it_is_taken(kvr, n_pages):
             assert refs[:3].tolist() == [2, 1, 2] and bool((refs[3:3 + n] == 1).all()) and not refs[3 + n:].any()
             assert torch.equal(table[1], torch.arange(n, device="cuda").int() + 3)
             assert bool((table[0] == -1).all()) and bool((table[2] == -1).all())
+
+
+@pytest.mark.parametrize("n_pages", [5, 5000])
+def test_copies_of_a_call_that_fails_for_another_row(kvr, n_pages):
+    """Three rows share a page and grow, one of them too far: the error brings the copies of the
+    others, whose pages have changed already."""
+    import torch
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    cache = kvr.LatentCache(torch.randn(n_pages, 16, 288, device="cuda").bfloat16(), 32)
+    refs, table, kv = ints(*[0] * n_pages), torch.full((3, n_pages), -1, dtype=torch.int32, device="cuda"), ints(0, 0, 0)
+    kvr.kvr_pages_resize(refs, table, kv, ints(20, 0, 0), 16)
+    kvr.kvr_pages_fork(refs, table, kv, ints(-1, 0, 0), 16)
+    with pytest.raises(kvr.KvrError) as e:
+        kvr.kvr_pages_resize(refs, table, kv, ints(21, 22, 16 * n_pages), 16)
+    assert e.value.code == kvr.KVR_E_DOMAIN
+    assert e.value.copies.tolist() == [[1, 2], [1, 3], [-1, -1]] and kv.tolist() == [21, 22, 20]
+    kvr.kvr_pages_copy(kvr.PageBuffers(cache), e.value.copies)
+    assert torch.equal(cache.rows[2], cache.rows[1]) and torch.equal(cache.rows[3], cache.rows[1])
+    kvr.kvr_pages_resize(refs, table, kv, ints(0, -1, -1), 16)   # a hole at 2
+    kv[0] = -1
+    with pytest.raises(kvr.KvrError) as e:
+        kvr.kvr_pages_compact(refs, table, kv, 16, max_moves=2)
+    assert e.value.moves.tolist() == [[3, 2], [-1, -1]] and e.value.used.tolist() == [3]
+    assert table[1, :2].tolist() == [0, 2]
+    with pytest.raises(kvr.KvrError) as e:   # refused on the host: nothing was done
+        kvr.kvr_pages_resize(refs, table, kv, ints(0, -1, -1), 15)
+    assert not hasattr(e.value, "copies")

@@ -239,18 +239,18 @@ struct LatentTile {
     }
 
     // 16-bit rows: wave `mover` brings every Movers-th KB of the latents, and the shared keys of
-    // parts mover, mover + Movers, ...: Loads loads, of which First to Last - 1 are made here.
+    // parts mover, mover + Movers, ...
     static constexpr int RowChunks = Rank / 8, TailChunks = 4 * RO;        // of a row
     static constexpr int RowsMain = 64 / RowChunks, RowsTail = 64 / TailChunks;   // of a load
     static constexpr int TailOf = 16 / RowsTail;                           // loads of a part's shared keys
     static constexpr int MainOf = Main / 1024 / Movers;
     static constexpr int Loads = MainOf + (Movers <= Parts ? Parts / Movers * TailOf : 1);
-    template <bool Whole, int First = 0, int Last = Loads>
+    template <bool Whole>
     __device__ __forceinline__ void fetch_rows(const Where &w, int mover, uint32_t tile) const
     {
         static_assert(Movers * RowsMain <= 16 && (Parts % Movers == 0 || (Parts == 4 && Movers == 8)), "whole parts");
         const uint32_t stride = (uint32_t)la.c.token_stride;
-        static_for<First, Last>([&](auto L) {
+        static_for<0, Loads>([&](auto L) {
             constexpr int l = decltype(L)::value;
             if constexpr (l < MainOf) {
                 constexpr int per = RowsMain > 1 ? RowChunks : 64;

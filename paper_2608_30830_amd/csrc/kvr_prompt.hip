@@ -6,7 +6,7 @@
 //
 // They compute S^T = K Q^T and O^T = V^T P^T (16x16x32), so that a lane owns one query (lane mod
 // 16) and P^T leaves the first product in the layout that the second one takes.  A block has
-// four waves of 16 RT queries of one head; 64 keys and values (a step) go from memory to LDS
+// four waves of 32 queries of one head; 64 keys and values (a step) go from memory to LDS
 // without passing through registers, while the step before is worked on, 16-byte chunks
 // exchanged within a row so that reading along it (keys) and across it (values, ds_read_b64_tr_b16)
 // spreads over the banks.  A causal block ends at the last key that its queries see, a wave at its
@@ -27,6 +27,7 @@ namespace kv {
 namespace {
 
 constexpr int kKeys = 64;   // of a step
+constexpr int kBlockRows = 128;   // queries of a block
 
 // LDS position of chunk c (16 bytes) of row r, rows of C chunks.
 template <int C>
@@ -83,11 +84,11 @@ __device__ __forceinline__ Item find_item(const Prompt &p, int item)
     return none;
 }
 
-template <int MT, int NOPE, int ROT, int RT>
+template <int MT, int NOPE, int ROT>
 struct PromptKernel {
     static constexpr int KB = NOPE / 32, SB = ROT / 32, NB = KB + SB;   // blocks of 32 elements
     static constexpr int VT = NOPE / 16;                                // value tiles
-    static constexpr int WaveRows = 16 * RT, BlockRows = 4 * WaveRows;
+    static constexpr int BlockRows = kBlockRows, WaveRows = BlockRows / 4, RT = WaveRows / 16;
     // LDS bytes of a step: own keys, shared keys, values
     static constexpr int OwnBytes = kKeys * NOPE * 2, SharedBytes = kKeys * ROT * 2;
     static constexpr int Tile = 2 * OwnBytes + SharedBytes, ValuesAt = OwnBytes + SharedBytes;
@@ -343,10 +344,10 @@ struct PromptKernel {
     }
 };
 
-template <int MT, int NOPE, int ROT, int RT>
-__global__ __launch_bounds__(256, RT > 2 ? 1 : 2) void prompt_kernel(Prompt p)
+template <int MT, int NOPE, int ROT>
+__global__ __launch_bounds__(256, 2) void prompt_kernel(Prompt p)
 {
-    using K = PromptKernel<MT, NOPE, ROT, RT>;
+    using K = PromptKernel<MT, NOPE, ROT>;
     __shared__ __align__(1024) char lds[K::LdsBytes];
     K k(p);
     k.run(lds);
@@ -390,12 +391,11 @@ __global__ __launch_bounds__(256) void join_kernel(Prompt p)
         p.lse[q * p.q_heads + h] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-template <int MT, int NOPE, int ROT, int RT>
+template <int MT, int NOPE, int ROT>
 hipError_t launch_rows(const Prompt &p, hipStream_t stream)
 {
-    if (p.block_rows != PromptKernel<MT, NOPE, ROT, RT>::BlockRows) return hipErrorInvalidValue;
     const int64_t blocks = (int64_t)p.max_items * p.q_heads;
-    prompt_kernel<MT, NOPE, ROT, RT><<<grid_of(blocks * p.parts), 256, 0, stream>>>(p);
+    prompt_kernel<MT, NOPE, ROT><<<grid_of(blocks * p.parts), 256, 0, stream>>>(p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts == 1) return e;
     join_kernel<MT, NOPE><<<grid_of(blocks * (p.block_rows / (1024 / NOPE))), 256, 0, stream>>>(p);
@@ -405,7 +405,7 @@ hipError_t launch_rows(const Prompt &p, hipStream_t stream)
 template <int MT, int NOPE>
 hipError_t launch_rot(const Prompt &p, hipStream_t stream)
 {
-    return p.rot == 64 ? launch_rows<MT, NOPE, 64, 2>(p, stream) : launch_rows<MT, NOPE, 32, 2>(p, stream);
+    return p.rot == 64 ? launch_rows<MT, NOPE, 64>(p, stream) : launch_rows<MT, NOPE, 32>(p, stream);
 }
 
 template <int MT>
@@ -420,7 +420,7 @@ constexpr int kSlots = 512;   // blocks that are resident at once
 
 size_t plan_prompt(Prompt &p)
 {
-    p.block_rows = 128;
+    p.block_rows = kBlockRows;
     // (with all heads at most 2^36 / 128 + 2^24)
     p.max_items = (int32_t)std::max<int64_t>(
         1, std::min<int64_t>((int64_t)p.n_seqs * cdiv(p.max_q, p.block_rows),

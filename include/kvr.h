@@ -578,7 +578,8 @@ typedef struct {
  *   d_key          device, dtype [n_tokens][rot], likewise.
  *   d_norm         device, dtype [rank], 16-byte aligned, or NULL (latents as they are);
  *                  eps finite and >= 0 (else KVR_E_GRID).
- *   d_slots, d_pos, d_table, n_pos, rot_dim, flags: as kvr_cache_write, rot_dim <= rot.
+ *   d_slots, d_pos, d_table, n_pos, rot_dim, flags: as kvr_cache_write, rot_dim <= rot.  A slot
+ *                  that is given twice in a call may hold parts of either row afterwards.
  */
 int kvr_latent_write(const kvr_latent_cache *cache, const void *d_latent, const void *d_key,
                      int32_t dtype, int64_t n_tokens, int64_t latent_stride, int64_t key_stride,

@@ -19,8 +19,8 @@ inline int chunk_words(int64_t n_pages)
     return words;
 }
 // Pools that one block goes through in one launch, for new lengths and for compaction.  (A call in a
-// graph, one launch against two or three: new lengths of 32 rows in 1,024 pages 5.7 us against 7.0, of 64
-// rows in 4,096 pages 7.9 against 7.1, in 16,384 16.7 against 8.0; compaction of 32 rows in 1,024 pages
+// graph, one launch against two or three: new lengths of 32 rows in 1,024 pages 5.8 us against 6.8, of 64
+// rows in 4,096 pages 8.0 against 7.3, of 16 in 16,384 15.1 against 8.6; compaction of 32 rows in 1,024 pages
 // 5.3 against 8.4, of 64 in 4,096 7.1 against 8.6, of 160 9.3 against 8.8, of 64 in 16,384 12.9 against 8.9.)
 constexpr int kSmallResize = 2048, kSmallSeqs = 1024, kSmallCompact = 4096, kFewSeqs = 64;
 constexpr int kSmallEntries = 65536;   // of all rows of the table

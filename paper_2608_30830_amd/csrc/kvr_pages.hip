@@ -48,7 +48,8 @@ __device__ __forceinline__ void give_back(const Pool &p, int page)
 }
 // Up to four entries, which become -1: the atomics of one wait together.  free: the pages that were
 // free when the call began, as bits.  What names one of them is reported, whether or not another row
-// has taken the page meanwhile, whose count it would lower.
+// has taken the page meanwhile, whose count it would lower.  (A load before each atomic: 64 rows in
+// 4,096 pages 7.1 us a call without it, 7.3 with it; one row of 6,144 pages 28.6 and 32.7.)
 __device__ __forceinline__ void give_back(const Pool &p, const uint64_t *free, int32_t *const (&at)[4])
 {
     int page[4], held[4];

@@ -14,8 +14,8 @@
 // keys of each are cut into parts, which join_kernel joins.  Scores, sums and outputs are held in 32
 // bits; weights are rounded to the inputs' type and the outputs divided by the sum of the rounded ones.
 //
-// One prompt of 8,192 tokens, 32 heads of 128 + 64: 711 us a call (670 to 750 by card), 967 TFLOP/s, where a
-// large product reaches 1,135.  Two chunks of 509 after 16,384 tokens: 273 us, 12 of them the joining.
+// One prompt of 8,192 tokens, 32 heads of 128 + 64: 690 us a call in a steady run (670 to 750 by card), 996
+// TFLOP/s, where a large product reaches 1,135; the first dozen calls after a pause take 770 to 950.  Two chunks of 509 after 16,384 tokens: 268 us, 12 of them the joining.
 // Fragments read in groups ahead of the products, as attention over latents does, spilled
 // registers: 967 against 805 us on the same card.
 #include <algorithm>
@@ -427,6 +427,10 @@ size_t plan_prompt(Prompt &p)
                              p.n_queries / p.block_rows + p.n_seqs));
     const int64_t blocks = (int64_t)p.max_items * p.q_heads;
     const int64_t steps = cdiv(p.max_k, kKeys);
+    // Parts of eight steps or more (us a call, joining included, against four or more: one head of 500 tokens
+    // 22 and 18, of 900 32 and 21, of 1,500 26 and 21, of 4,000 33 and 35; eight heads of 900 33 and 25, of
+    // 1,500 33 and 35; 32 heads of 500 22 and 26, of 900 34 and 42; two chunks of 509 behind a long past
+    // alike): eight favours many heads, four would favour the few.
     p.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kSlots / blocks, steps / 8));
     if (p.parts == 1) return 0;
     return (size_t)p.parts * blocks * p.block_rows * (p.nope + 4) * sizeof(float);

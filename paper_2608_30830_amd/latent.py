@@ -121,7 +121,7 @@ def kvr_latent_write(cache: LatentCache, latent, key, slots, positions=None, tab
                      norm_weight=None, eps: float = 1e-6, interleaved: bool = False,
                      adjoint: bool = False, status=None, stream=None, check: bool = True) -> None:
     """latent [tokens, rank] and key [tokens, rot] into ``slots`` [tokens] int64 (page *
-    page_size + row; below 0: not written).  With ``norm_weight`` [rank] (of the latents' type)
+    page_size + row; below 0: not written; each once).  With ``norm_weight`` [rank] (of the latents' type)
     latents are normalised, c w / sqrt(mean(c^2) + eps); with ``table`` keys are rotated by
     ``positions``; both in 32 bits on the way."""
     c = kv._context()
